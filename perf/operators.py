@@ -1,0 +1,509 @@
+"""Operators at the ends of a pipeline stage: what a stage computes right after it has received a message and right before
+it sends one, as calls of the library (`own`) and in plain form.
+
+  norm          residual addition and root-mean-square norm of the rows that arrive, with an output in 8 bits and a scale a
+                row where the next product reads 8 bits: out of a message's packed buffer (with its checksums), or of tensors
+  norm_grad     its gradient, written into the message that goes back to the stage before, and the weight's
+  product       matrix product with bias, activation and residual in its epilogue, bf16 or 8-bit factors, into a tensor or
+                straight into the message that leaves the stage
+  product_grad  its gradients: before the activation, of both factors and of the bias
+
+Sizes come from the boundary messages in paper_2602_18007_amd/workloads.py (4096 tokens of 4096 elements, 8192 of 3584, the
+small one of 128 x 512) and the weight gradients it lists (14336 x 4096); draw() spreads them over the ranges these stand for.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+EPS = 1e-5
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+ESIZE = {"bf16": 2, "f32": 4, "e4m3": 1}
+E4M3_MAX, TINY = 448.0, 2.0 ** -126
+MOST_PRODUCT = 4096 * 4096 * 14336
+MOST_ROWS = 8192 * 8192
+
+
+# ---- the cases ----------------------------------------------------------------------
+
+def listed():
+    return [
+        # One token of a decode step reaches a stage, hidden state and residual in one message: latency counts.
+        dict(name="norm_token", op="norm", message=True, rows=1, cols=4096, dtype="bf16", residual="message", h=True, y=False,
+             q=True, sums=True, lanes=1, chunk_kib=16, pad=0),
+        # The boundary's activation with its residual, for a first layer that works in 8 bits.
+        dict(name="norm_boundary_8bit", op="norm", message=True, rows=4096, cols=4096, dtype="bf16", residual="message", h=True,
+             y=False, q=True, sums=True, lanes=4, chunk_kib=1024, pad=0),
+        # Two sequences of a 7B model's activation added to what the stage holds, normed in bf16; rows cross chunks.
+        dict(name="norm_two_sequences", op="norm", message=True, rows=8192, cols=3584, dtype="bf16", residual="local", h=True,
+             y=True, q=False, sums=True, lanes=8, chunk_kib=4096, pad=0),
+        # Ragged f32 rows inside a wider buffer, no message.
+        dict(name="norm_ragged_f32", op="norm", message=False, rows=1021, cols=1003, dtype="f32", residual="local", h=False,
+             y=True, q=True, sums=False, lanes=1, chunk_kib=256, pad=5),
+        # Backward of the boundary's norm: the gradient goes straight into the message for the stage before.
+        dict(name="norm_grad_boundary", op="norm_grad", message=True, rows=4096, cols=4096, dtype="bf16", dh=True, lanes=4,
+             chunk_kib=1024, pad=0),
+        # The small activation's backward, in f32.
+        dict(name="norm_grad_small", op="norm_grad", message=False, rows=128, cols=512, dtype="f32", dh=True, lanes=2,
+             chunk_kib=16, pad=0),
+        # One token through the projection that ends a stage: the weight is read once.
+        dict(name="product_token", op="product", message=True, m=1, n=4096, k=14336, dtype="bf16", out="bf16", bias=False,
+             act="none", residual=True, pre=False, lanes=1, chunk_kib=16, pad=0),
+        # A decode batch that is no whole number of tiles, in 8 bits.
+        dict(name="product_batch_8bit", op="product", message=False, m=61, n=14336, k=4096, dtype="e4m3", out="bf16", bias=False,
+             act="silu", residual=False, pre=False, lanes=1, chunk_kib=256, pad=0),
+        # The projection that ends a stage, with the residual, into the boundary's message.
+        dict(name="product_boundary", op="product", message=True, m=4096, n=4096, k=14336, dtype="bf16", out="bf16", bias=False,
+             act="none", residual=True, pre=False, lanes=4, chunk_kib=1024, pad=0),
+        # The projection that reads the norm's 8 bits, with what its gradient needs kept.
+        dict(name="product_first_8bit", op="product", message=False, m=4096, n=14336, k=4096, dtype="e4m3", out="bf16", bias=True,
+             act="gelu", residual=False, pre=True, lanes=1, chunk_kib=256, pad=0),
+        # Its backward pass in training: all gradients.
+        dict(name="product_grad_first", op="product_grad", m=4096, n=14336, k=4096, act="gelu", bias=True, db="bf16",
+             accumulate=False, pad=0),
+        # Odd sizes and padded rows, added to f32 weight gradients over micro-batches.
+        dict(name="product_grad_ragged", op="product_grad", m=1021, n=1000, k=515, act="none", bias=True, db="f32",
+             accumulate=True, pad=3),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi):
+    """Mostly whole vectors, as models have them, sometimes any number."""
+    v = _log(rng, lo, hi)
+    return v if rng.random() < 0.3 or v < 16 else v // 8 * 8
+
+
+def draw(rng):
+    lanes, chunk_kib = rng.choice([1, 2, 4, 8]), rng.choice([16, 64, 256, 1024, 4096])
+    op = rng.choice(["norm", "norm_grad", "product", "product", "product_grad"])
+    pad = rng.choice([0, 0, 8, 1])
+    if op in ("norm", "norm_grad"):
+        cols = _size(rng, 64, 8192)
+        rows = _log(rng, 1, min(8192, MOST_ROWS // cols))
+        dtype, message = rng.choice(["bf16", "bf16", "f32"]), rng.random() < 0.6
+        if op == "norm_grad":
+            return dict(op=op, message=message, rows=rows, cols=cols, dtype=dtype, dh=rng.random() < 0.7, lanes=lanes,
+                        chunk_kib=chunk_kib, pad=pad)
+        y = rng.random() < 0.5
+        return dict(op=op, message=message, rows=rows, cols=cols, dtype=dtype,
+                    residual=rng.choice(["message", "local", "none"] if message else ["local", "none"]), h=rng.random() < 0.7, y=y,
+                    q=not y or rng.random() < 0.4, sums=message and rng.random() < 0.7, lanes=lanes, chunk_kib=chunk_kib, pad=pad)
+    n, k = _size(rng, 64, 14336), _size(rng, 64, 14336)
+    m = _log(rng, 1, min(8192, max(1, MOST_PRODUCT // (n * k))))
+    act, bias = rng.choice(["none", "relu", "gelu", "silu"]), rng.random() < 0.5
+    if op == "product_grad":
+        db = "bf16" if act != "none" else rng.choice(["bf16", "f32"])
+        return dict(op=op, m=m, n=n, k=k, act=act, bias=bias, db=db, accumulate=rng.random() < 0.4, pad=pad)
+    message = rng.random() < 0.4
+    return dict(op=op, message=message, m=m, n=n, k=k, dtype=rng.choice(["bf16", "bf16", "e4m3"]),
+                out=rng.choice(["bf16", "bf16", "f32"]), bias=bias, act=act, residual=rng.random() < 0.5, pre=rng.random() < 0.3,
+                lanes=lanes, chunk_kib=chunk_kib, pad=pad)
+
+
+# ---- what a program has in hand -------------------------------------------------------
+
+class _Inputs:
+    def __init__(self, seed):
+        self.g = torch.Generator(device=DEV)
+        self.g.manual_seed(int(seed) & 0x7FFFFFFFFFFFFFFF)
+
+    def normal(self, rows, cols, std, dtype, pad=0):
+        """[rows, cols] values inside rows of cols + pad elements."""
+        x = torch.empty(rows, cols + pad, dtype=torch.float32, device=DEV).normal_(0.0, std, generator=self.g)
+        return x.to(dtype)[:, :cols]
+
+    def vector(self, n, mean, std, dtype=torch.float32):
+        return (mean + std * torch.empty(n, dtype=torch.float32, device=DEV).normal_(0.0, 1.0, generator=self.g)).to(dtype)
+
+    def activation(self, rows, cols, std, dtype, pad=0):
+        """Rows of differing size with a few channels far above the others, as residual streams have them."""
+        x = self.normal(rows, cols + pad, std, torch.float32)
+        x *= torch.exp(0.5 * self.vector(rows, 0.0, 1.0))[:, None]
+        x[:, :: max(1, cols // 4)] *= 12.0
+        return x.to(dtype)[:, :cols]
+
+    def eight_bits(self, rows, cols, std, pad=0):
+        x = self.normal(rows, cols + pad, std, torch.float32)
+        scale = (x.abs().amax(1) / E4M3_MAX).clamp_min(TINY)
+        return (x / scale[:, None]).to(torch.float8_e4m3fn)[:, :cols], scale
+
+
+def _up(n, to):
+    return (n + to - 1) // to * to
+
+
+class _Layout:
+    """Where a message's chunks lie in its packed buffer: chunk c in slot c // lanes of lane c % lanes, lanes one after another."""
+
+    def __init__(self, sizes, case):
+        self.lanes, self.chunk = case["lanes"], case["chunk_kib"] * 1024
+        self.starts, self.sizes, end = [], sizes, 0
+        for n in sizes:
+            self.starts.append(end)
+            end += _up(n, 256)
+        self.count = _up(end, self.chunk) // self.chunk
+        c = torch.arange(self.count, device=DEV)
+        lane, base, rest = c % self.lanes, self.count // self.lanes, self.count % self.lanes
+        self.place = lane * base + lane.clamp_max(rest) + c // self.lanes
+
+    def pack(self, tensors):
+        stream = torch.zeros(self.count * self.chunk, dtype=torch.uint8, device=DEV)
+        for at, t in zip(self.starts, tensors):
+            raw = t.contiguous().view(-1).view(torch.uint8)
+            stream[at:at + raw.numel()] = raw
+        packed = torch.empty(self.count, self.chunk, dtype=torch.uint8, device=DEV)
+        packed[self.place] = stream.view(self.count, self.chunk)
+        return packed.view(-1)
+
+    def unpack(self, packed, dtype, shape):
+        stream = packed.view(self.count, self.chunk)[self.place].view(-1)
+        return [stream[at:at + n].view(dtype).view(shape) for at, n in zip(self.starts, self.sizes)]
+
+    def sums(self, packed):
+        words = packed.view(self.count, self.chunk)[self.place].view(torch.int32).to(torch.int64) & 0xFFFFFFFF
+        return words.sum(1)
+
+
+def prepare(case, seed):
+    s = {"norm": _prepare_norm, "norm_grad": _prepare_norm_grad, "product": _prepare_product,
+         "product_grad": _prepare_product_grad}[case["op"]](case, _Inputs(seed))
+    s["case"] = case
+    if own:
+        _prepare_calls(s)
+    return s
+
+
+def _prepare_norm(case, make):
+    rows, cols, dt, pad = case["rows"], case["cols"], DTYPES[case["dtype"]], case["pad"]
+    in_message = case["message"]
+    x = make.activation(rows, cols, 1.0, dt, 0 if in_message else pad)
+    r = make.activation(rows, cols, 2.0, dt, 0 if case["residual"] == "message" else pad) if case["residual"] != "none" else None
+    s = dict(weight=make.vector(cols, 1.0, 0.2, dt))
+    if in_message:
+        n = rows * cols * ESIZE[case["dtype"]]
+        tensors = [x, r] if case["residual"] == "message" else [x]
+        s["layout"] = _Layout([n] * len(tensors), case)
+        s["packed"] = s["layout"].pack(tensors)
+    else:
+        s["x"] = x
+    s["residual"] = r if case["residual"] == "local" else None
+    return s
+
+
+def _prepare_norm_grad(case, make):
+    rows, cols, dt, pad = case["rows"], case["cols"], DTYPES[case["dtype"]], case["pad"]
+    s = dict(weight=make.vector(cols, 1.0, 0.2, dt), h=make.activation(rows, cols, 2.0, dt, pad),
+             dy=make.normal(rows, cols, 0.02, dt, pad), dh=make.normal(rows, cols, 0.02, dt, pad) if case["dh"] else None)
+    if case["message"]:
+        s["layout"] = _Layout([rows * cols * ESIZE[case["dtype"]]], case)
+    return s
+
+
+def _prepare_product(case, make):
+    m, n, k, pad, out = case["m"], case["n"], case["k"], case["pad"], DTYPES[case["out"]]
+    s = dict(a_scale=None, b_scale=None)
+    if case["dtype"] == "e4m3":
+        s["a"], s["a_scale"] = make.eight_bits(m, k, 1.0, pad)
+        s["b"], s["b_scale"] = make.eight_bits(n, k, 1.0 / math.sqrt(k), pad)
+    else:
+        s["a"], s["b"] = make.normal(m, k, 1.0, torch.bfloat16, pad), make.normal(n, k, 1.0 / math.sqrt(k), torch.bfloat16, pad)
+    s["bias"] = make.vector(n, 0.0, 0.5, torch.bfloat16) if case["bias"] else None
+    s["residual"] = make.activation(m, n, 1.0, out, pad) if case["residual"] else None
+    if case["message"]:
+        s["layout"] = _Layout([m * n * ESIZE[case["out"]]], case)
+    return s
+
+
+def _prepare_product_grad(case, make):
+    m, n, k, pad = case["m"], case["n"], case["k"], case["pad"]
+    s = dict(dc=make.normal(m, n, 0.02, torch.bfloat16, pad), a=make.normal(m, k, 1.0, torch.bfloat16, pad),
+             b=make.normal(n, k, 1.0 / math.sqrt(k), torch.bfloat16, pad),
+             pre=make.normal(m, n, 1.0, torch.bfloat16, pad) if case["act"] != "none" else None)
+    if case["accumulate"]:           # what earlier micro-batches have left
+        s["db0"] = make.normal(n, k, 0.5, DTYPES[case["db"]])
+        s["dbias0"] = make.vector(n, 0.0, 0.5)
+    return s
+
+
+# ---- the library's calls --------------------------------------------------------------
+
+def _empty(rows, cols, dtype):
+    return torch.empty(rows, cols, dtype=dtype, device=DEV)
+
+
+def _prepare_calls(s):
+    """The plan, the output buffers and the argument blocks that a program keeps over its steps."""
+    from paper_2602_18007_amd import hxt
+    case, op = s["case"], s["case"]["op"]
+    if case.get("message"):
+        rows, cols, dt = (case["m"], case["n"], case["out"]) if op == "product" else (case["rows"], case["cols"], case["dtype"])
+        shape = ((rows, cols), None, DTYPES[dt])
+        s["plan"] = hxt.hxt_plan_multi([shape] * len(s["layout"].sizes), case["lanes"], case["chunk_kib"] * 1024)
+        if op != "norm":
+            s["packed"] = torch.zeros(s["plan"].packed_bytes, dtype=torch.uint8, device=DEV)
+    if op == "norm":
+        rows, cols, dt = case["rows"], case["cols"], DTYPES[case["dtype"]]
+        out = dict(h=_empty(rows, cols, dt) if case["h"] else None, y=_empty(rows, cols, dt) if case["y"] else None)
+        if case["q"]:
+            out["q"], out["scale"] = _empty(rows, cols, torch.float8_e4m3fn), torch.empty(rows, dtype=torch.float32, device=DEV)
+        if case["sums"]:
+            s["sums"] = torch.empty(s["plan"].num_chunks, dtype=torch.int64, device=DEV)
+        s["out"] = {name: t for name, t in out.items() if t is not None}
+        s["call"] = hxt.Norm(s["weight"], EPS, x=s.get("x"), residual=s["residual"], **s["out"])
+    elif op == "norm_grad":
+        rows, cols = case["rows"], case["cols"]
+        work = torch.empty(hxt.hxt_norm_grad_work_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+        s["out"] = dict(dweight=torch.empty(cols, dtype=torch.float32, device=DEV))
+        if not case["message"]:
+            s["out"]["dx"] = _empty(rows, cols, DTYPES[case["dtype"]])
+        s["call"] = hxt.NormGrad(s["weight"], EPS, h=s["h"], dy=s["dy"], dh=s["dh"], work=work, **s["out"])
+    elif op == "product":
+        m, n, k = case["m"], case["n"], case["k"]
+        work = torch.empty(hxt.hxt_product_work_bytes(m, n, k, DTYPES[case["dtype"]]), dtype=torch.uint8, device=DEV)
+        s["out"] = dict(pre=_empty(m, n, torch.bfloat16)) if case["pre"] else {}
+        if not case["message"]:
+            s["out"]["c"] = _empty(m, n, DTYPES[case["out"]])
+        s["call"] = hxt.Product(s["a"], s["b"], a_scale=s["a_scale"], b_scale=s["b_scale"], bias=s["bias"], act=case["act"],
+                                residual=s["residual"], work=work, out_dtype=DTYPES[case["out"]], **s["out"])
+    else:
+        m, n, k = case["m"], case["n"], case["k"]
+        work = torch.empty(hxt.hxt_product_grad_work_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+        s["out"] = dict(da=_empty(m, k, torch.bfloat16), db=_empty(n, k, DTYPES[case["db"]]))
+        if case["bias"]:
+            s["out"]["dbias"] = torch.empty(n, dtype=torch.float32, device=DEV)
+        if case["act"] != "none":
+            s["out"]["dz"] = _empty(m, n, torch.bfloat16)
+        s["call"] = hxt.ProductGrad(s["dc"], s["a"], s["b"], pre=s["pre"], act=case["act"], work=work, db_add=s.get("db0"),
+                                    dbias_add=s.get("dbias0") if case["bias"] else None, **s["out"])
+
+
+def _call(s):
+    from paper_2602_18007_amd import hxt
+    case, op = s["case"], s["case"]["op"]
+    if op == "norm":
+        if not case["message"]:
+            hxt.hxt_norm(s["call"])
+            return s["out"]
+        hxt.hxt_unpack_norm(s["plan"], s["packed"], s["call"], s.get("sums"))
+        return dict(s["out"], sums=s["sums"]) if case["sums"] else s["out"]
+    if op == "product_grad":
+        hxt.hxt_product_grad(s["call"])
+        return s["out"]
+    if not case["message"]:
+        (hxt.hxt_norm_grad if op == "norm_grad" else hxt.hxt_product)(s["call"])
+        return s["out"]
+    (hxt.hxt_pack_norm_grad if op == "norm_grad" else hxt.hxt_pack_product)(s["plan"], s["call"], s["packed"])
+    return dict(s["out"], packed=s["packed"].view(DTYPES[case["dtype"] if op == "norm_grad" else case["out"]]))
+
+
+# ---- the plain form -------------------------------------------------------------------
+
+def run(s):
+    if own:
+        return _call(s)
+    return {"norm": _norm, "norm_grad": _norm_grad, "product": _product, "product_grad": _product_grad}[s["case"]["op"]](s)
+
+
+def _norm(s):
+    case = s["case"]
+    dt, out = DTYPES[case["dtype"]], {}
+    if case["message"]:
+        tensors = s["layout"].unpack(s["packed"], dt, (case["rows"], case["cols"]))
+        x, r = tensors[0], tensors[1] if len(tensors) > 1 else s["residual"]
+        if case["sums"]:
+            out["sums"] = s["layout"].sums(s["packed"])
+    else:
+        x, r = s["x"], s["residual"]
+    h = x.float()
+    if r is not None:
+        h = h + r.float()
+    y = h * torch.rsqrt((h * h).mean(1, keepdim=True) + EPS) * s["weight"].float()
+    if case["h"]:
+        out["h"] = h.to(dt)
+    if case["y"]:
+        out["y"] = y.to(dt)
+    if case["q"]:
+        scale = (y.abs().amax(1) / E4M3_MAX).clamp_min(TINY)
+        out["q"], out["scale"] = (y / scale[:, None]).to(torch.float8_e4m3fn), scale
+    return out
+
+
+def _norm_grad(s):
+    case = s["case"]
+    h, dy = s["h"].float(), s["dy"].float()
+    rstd = torch.rsqrt((h * h).mean(1, keepdim=True) + EPS)
+    n, g = h * rstd, dy * s["weight"].float()
+    dx = rstd * (g - n * (g * n).mean(1, keepdim=True))
+    if s["dh"] is not None:
+        dx = dx + s["dh"].float()
+    dx, dweight = dx.to(DTYPES[case["dtype"]]), (dy * n).sum(0)
+    if case["message"]:
+        return dict(dweight=dweight, packed=s["layout"].pack([dx]).view(dx.dtype))
+    return dict(dweight=dweight, dx=dx)
+
+
+GELU_A, GELU_B = math.sqrt(2.0 / math.pi), 0.044715
+
+
+def _act(z, act):
+    if act == "relu":
+        return z * (z > 0)
+    if act == "silu":
+        return z / (1 + torch.exp(-z))
+    if act == "gelu":
+        return 0.5 * z * (1 + torch.tanh(GELU_A * (z + GELU_B * z * z * z)))
+    return z
+
+
+def _act_grad(z, act):
+    if act == "relu":
+        return (z > 0).to(z.dtype)
+    if act == "silu":
+        e = 1 / (1 + torch.exp(-z))
+        return e * (1 + z * (1 - e))
+    t = torch.tanh(GELU_A * (z + GELU_B * z * z * z))
+    return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * GELU_A * (1 + 3 * GELU_B * z * z)
+
+
+def _product(s):
+    case, out = s["case"], {}
+    z = s["a"].float() @ s["b"].float().t()
+    if s["a_scale"] is not None:
+        z = z * s["a_scale"][:, None] * s["b_scale"][None, :]
+    if s["bias"] is not None:
+        z = z + s["bias"].float()
+    if case["pre"]:
+        out["pre"] = z.to(torch.bfloat16)
+    c = _act(z, case["act"])
+    if s["residual"] is not None:
+        c = c + s["residual"].float()
+    c = c.to(DTYPES[case["out"]])
+    if case["message"]:
+        out["packed"] = s["layout"].pack([c]).view(c.dtype)
+    else:
+        out["c"] = c
+    return out
+
+
+def _product_grad(s):
+    case, out = s["case"], {}
+    dz = s["dc"].float()
+    if case["act"] != "none":
+        dz = dz * _act_grad(s["pre"].float(), case["act"])
+        out["dz"] = dz.to(torch.bfloat16)
+    db, dbias = dz.t() @ s["a"].float(), dz.sum(0)
+    if case["accumulate"]:
+        db, dbias = s["db0"].float() + db, s["dbias0"] + dbias
+    out["da"], out["db"] = (dz @ s["b"].float()).to(torch.bfloat16), db.to(DTYPES[case["db"]])
+    if case["bias"]:
+        out["dbias"] = dbias
+    return out
+
+
+# ---- what a pass cannot do without ------------------------------------------------------
+
+def work(case):
+    op = case["op"]
+    if op in ("norm", "norm_grad"):
+        e, es = case["rows"] * case["cols"], ESIZE[case["dtype"]]
+        if op == "norm":
+            moved = es * (1 + (case["residual"] != "none") + case["h"] + case["y"]) + case["q"]
+            return {"bytes": e * moved + case["cols"] * es + 4 * case["rows"] * case["q"], "flops": 6 * e}
+        return {"bytes": e * es * (3 + case["dh"]) + case["cols"] * (es + 4), "flops": 12 * e}
+    m, n, k = case["m"], case["n"], case["k"]
+    if op == "product":
+        es, eo = ESIZE[case["dtype"]], ESIZE[case["out"]]
+        return {"bytes": es * (m * k + n * k) + eo * m * n * (1 + case["residual"]) + 2 * m * n * case["pre"] + 2 * n * case["bias"],
+                "flops": 2 * m * n * k}
+    act, edb = case["act"] != "none", ESIZE[case["db"]]
+    return {"bytes": 2 * (m * n * (1 + 2 * act) + 2 * m * k + n * k) + edb * n * k * (1 + case["accumulate"]) + 4 * n * case["bias"],
+            "flops": 4 * m * n * k}
+
+
+# ---- the definitions in 64 bits -----------------------------------------------------------
+
+def exact(case, seed):
+    """What the formulas give for the prepared inputs, laid out as run() does, every step in 64 bits."""
+    s = prepare(case, seed)
+    f64 = lambda t: t.to(torch.float64)                                      # noqa: E731
+    op, out = case["op"], {}
+
+    def message(t):
+        """t's values where the packed buffer has them, zeros elsewhere."""
+        per = case["chunk_kib"] * 1024 // ESIZE[case["out"] if op == "product" else case["dtype"]]
+        chunks = -(-t.numel() // per)
+        flat = torch.zeros(chunks * per, dtype=torch.float64, device=DEV)
+        flat[:t.numel()] = t.reshape(-1)
+        order = [c for lane in range(case["lanes"]) for c in range(lane, chunks, case["lanes"])]
+        return flat.view(chunks, per)[torch.tensor(order, device=DEV)].view(-1)
+
+    if op == "norm":
+        dt, shape = DTYPES[case["dtype"]], (case["rows"], case["cols"])
+        if case["message"]:
+            got = s["layout"].unpack(s["packed"], dt, shape)
+            x, r = got[0], (got[1] if case["residual"] == "message" else s["residual"])
+            if case["sums"]:
+                out["sums"] = None
+        else:
+            x, r = s["x"], s["residual"]
+        h = f64(x) if r is None else f64(x) + f64(r)
+        y = f64(s["weight"]) * h / torch.sqrt(EPS + h.square().sum(1, keepdim=True) / case["cols"])
+        scale = torch.clamp_min(y.abs().max(1).values / E4M3_MAX, TINY)
+        for name, v in (("h", h), ("y", y), ("q", y / scale.unsqueeze(1))):
+            if case[name]:
+                out[name] = v
+        if case["q"]:
+            out["scale"] = scale
+        return out
+    if op == "norm_grad":
+        h, dy, w = f64(s["h"]), f64(s["dy"]), f64(s["weight"])
+        ms = EPS + h.square().sum(1, keepdim=True) / case["cols"]
+        dx = dy * w / ms.sqrt() - h * ((dy * w * h).sum(1, keepdim=True) / case["cols"]) / (ms * ms.sqrt())
+        if case["dh"]:
+            dx = dx + f64(s["dh"])
+        out["dweight"] = (dy * h / ms.sqrt()).sum(0)
+        out["packed" if case["message"] else "dx"] = message(dx) if case["message"] else dx
+        return out
+
+    def curve(z):
+        """The activation and its derivative."""
+        if case["act"] == "relu":
+            return torch.clamp_min(z, 0), (z > 0).double()
+        if case["act"] == "silu":
+            sig = torch.sigmoid(z)
+            return z * sig, sig + z * sig * (1 - sig)
+        if case["act"] == "gelu":                  # z * sigmoid(2u) is z/2 (1 + tanh u)
+            u2 = 2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)
+            sig = torch.sigmoid(u2)
+            return z * sig, sig + z * sig * (1 - sig) * 2 * math.sqrt(2 / math.pi) * (1 + 0.134145 * z * z)
+        return z, torch.ones_like(z)
+
+    if op == "product":
+        z = torch.matmul(f64(s["a"]), f64(s["b"]).t().contiguous())
+        if case["dtype"] == "e4m3":
+            z = z * torch.outer(f64(s["a_scale"]), f64(s["b_scale"]))
+        if case["bias"]:
+            z = z + f64(s["bias"])
+        if case["pre"]:
+            out["pre"] = z
+        c = curve(z)[0]
+        if case["residual"]:
+            c = c + f64(s["residual"])
+        out["packed" if case["message"] else "c"] = message(c) if case["message"] else c
+        return out
+    dz = f64(s["dc"]) if case["act"] == "none" else f64(s["dc"]) * curve(f64(s["pre"]))[1]
+    if case["act"] != "none":
+        out["dz"] = dz
+    out["da"] = torch.matmul(dz, f64(s["b"]))
+    out["db"] = torch.matmul(dz.t().contiguous(), f64(s["a"])) + (f64(s["db0"]) if case["accumulate"] else 0)
+    if case["bias"]:
+        out["dbias"] = dz.sum(0) + (f64(s["dbias0"]) if case["accumulate"] else 0)
+    return out
