@@ -103,9 +103,9 @@ def draw(rng):
         db = "bf16" if act != "none" else rng.choice(["bf16", "f32"])
         return dict(op=op, m=m, n=n, k=k, act=act, bias=bias, db=db, accumulate=rng.random() < 0.4, pad=pad)
     message = rng.random() < 0.4
-    return dict(op=op, message=message, m=m, n=n, k=k, dtype=rng.choice(["bf16", "bf16", "e4m3"]),
-                out=rng.choice(["bf16", "bf16", "f32"]), bias=bias, act=act, residual=rng.random() < 0.5, pre=rng.random() < 0.3,
-                lanes=lanes, chunk_kib=chunk_kib, pad=pad)
+    dtype = rng.choice(["bf16", "bf16", "e4m3"])        # products of 8 bits are worth 16
+    return dict(op=op, message=message, m=m, n=n, k=k, dtype=dtype, out="bf16" if dtype == "e4m3" else rng.choice(["bf16", "bf16", "f32"]),
+                bias=bias, act=act, residual=rng.random() < 0.5, pre=rng.random() < 0.3, lanes=lanes, chunk_kib=chunk_kib, pad=pad)
 
 
 # ---- what a program has in hand -------------------------------------------------------
