@@ -20,6 +20,7 @@
 #include "hxt_internal.h"
 #include "hxt_kernels.h"
 #include "hxt_launch.h"
+#include "hxt_operators.h"
 #include "hxt_rules.h"
 
 using namespace hxt;
@@ -703,6 +704,22 @@ int run_batch(int n, const hxt_plan_t *const *plans, void *const *const *tensors
         HXT_HIP(hipGetLastError());
         i = j;
     }
+    return HXT_OK;
+}
+
+// One pass over a packed buffer that sums its chunks.
+int checksum_pass(hxt_plan_t &pl, const uint8_t *pk, uint64_t *sums, Op op, hipStream_t st)
+{
+    SumCtx cx{nullptr, nullptr, 0, 0, 1, 0};
+    SlotsLock lock(pl.slots_mu);
+    const int rc = claim_slots(pl, op, st, cx, sums);
+    if (rc != HXT_OK) return rc;
+    cx.sum_bits = pl.sum_bits_geom;
+    if (pass_nontemporal(pl.nt_packed, launch_bytes(pl.p)))
+        k_checksum<true><<<pl.p.geom.ntiles, kThreads, 0, st>>>(pl.p.geom, pk, cx);
+    else
+        k_checksum<false><<<pl.p.geom.ntiles, kThreads, 0, st>>>(pl.p.geom, pk, cx);
+    HXT_HIP(hipGetLastError());
     return HXT_OK;
 }
 
@@ -1473,19 +1490,7 @@ int hxt_checksum(const hxt_plan_t *plan, const void *packed, uint64_t *sums, voi
     int rc = check_common(plan, packed);
     if (rc != HXT_OK || plan->p.C == 0) return rc;
     if (!sums) return HXT_EINVAL;
-    hxt_plan_t &pl = *const_cast<hxt_plan_t *>(plan);
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    SumCtx cx{nullptr, nullptr, 0, 0, 1, 0};
-    SlotsLock lock(pl.slots_mu);
-    if ((rc = claim_slots(pl, OP_CHECKSUM, st, cx, sums)) != HXT_OK) return rc;
-    cx.sum_bits = pl.sum_bits_geom;
-    const uint8_t *pk = static_cast<const uint8_t *>(packed);
-    if (pass_nontemporal(pl.nt_packed, launch_bytes(pl.p)))
-        k_checksum<true><<<pl.p.geom.ntiles, kThreads, 0, st>>>(pl.p.geom, pk, cx);
-    else
-        k_checksum<false><<<pl.p.geom.ntiles, kThreads, 0, st>>>(pl.p.geom, pk, cx);
-    HXT_HIP(hipGetLastError());
-    return HXT_OK;
+    return checksum_pass(*const_cast<hxt_plan_t *>(plan), static_cast<const uint8_t *>(packed), sums, OP_CHECKSUM, static_cast<hipStream_t>(stream));
 }
 
 
@@ -1595,3 +1600,41 @@ int hxt_last_hip_error(void) { return g_last_hip; }
 const char *hxt_version(void) { return "hxt 0.4 (gfx950)"; }
 
 }  // extern "C"
+
+// ---- what the operators at the ends of a stage borrow (hxt_operators.h) -----------------------
+
+namespace hxt {
+
+int operator_fail(hipError_t e) { return hip_fail(e); }
+
+int operator_device()
+{
+    int cur = -1;
+    const hipError_t e = hipGetDevice(&cur);
+    if (e == hipSuccess) return HXT_OK;
+    (void)hipGetLastError();
+    return hip_fail(e);
+}
+
+int operator_message(const hxt_plan_t *plan, const void *packed) { return check_common(plan, packed); }
+
+const Plan &operator_plan(const hxt_plan_t *plan) { return plan->p; }
+
+int operator_sums(const hxt_plan_t *plan, const void *packed, uint64_t *sums, bool send, hipStream_t st)
+{
+    return checksum_pass(*const_cast<hxt_plan_t *>(plan), static_cast<const uint8_t *>(packed), sums, send ? OP_PACK : OP_UNPACK, st);
+}
+
+int operator_unpack_sums(const hxt_plan_t *plan, uint64_t *sums, hipStream_t st, void (*enqueue)(void *ctx, const SumCtx &cx), void *ctx)
+{
+    hxt_plan_t &pl = *const_cast<hxt_plan_t *>(plan);
+    SumCtx cx{nullptr, nullptr, 0, 0, 1, 0};
+    SlotsLock lock(pl.slots_mu);
+    const int rc = claim_slots(pl, OP_UNPACK, st, cx, sums);
+    if (rc != HXT_OK) return rc;
+    enqueue(ctx, cx);
+    HXT_HIP(hipGetLastError());
+    return HXT_OK;
+}
+
+}  // namespace hxt

@@ -57,6 +57,7 @@ static int dtype_size(hxt_dtype_t dt)
     case HXT_BF16: return 2;
     case HXT_F32: return 4;
     case HXT_F64: return 8;
+    case HXT_E4M3: break;
     }
     return 0;
 }

@@ -19,7 +19,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libhxt.so")
 
 HXT_OK, HXT_EINVAL, HXT_EALIGN, HXT_EUNSUPPORTED, HXT_EOVERLAP, HXT_EHIP, HXT_ENOMEM = 0, -1, -2, -3, -4, -5, -6
-HXT_U8, HXT_F16, HXT_BF16, HXT_F32, HXT_F64 = 1, 2, 3, 4, 5
+HXT_U8, HXT_F16, HXT_BF16, HXT_F32, HXT_F64, HXT_E4M3 = 1, 2, 3, 4, 5, 16
 HXT_MAX_DIMS = 8
 KIND_NAMES = {0: "none", 1: "contig", 2: "rows", 3: "transpose", 4: "generic", 6: "rows_split", 7: "transpose_span"}
 
@@ -33,6 +33,8 @@ EXPORTS = (
     "hxt_host_forward", "hxt_stage_hop", "hxt_checksum2", "hxt_seal", "hxt_verify", "hxt_pack_seal", "hxt_unpack_verify",
     "hxt_pack_noalloc", "hxt_plan_set_option", "hxt_pack_seal_batch", "hxt_unpack_verify_batch",
     "hxt_stage_d2h_slots", "hxt_stage_h2d_slots", "hxt_unpack_accumulate_batch",
+    "hxt_norm", "hxt_unpack_norm", "hxt_norm_grad", "hxt_pack_norm_grad", "hxt_norm_grad_work_bytes",
+    "hxt_product", "hxt_pack_product", "hxt_product_grad", "hxt_product_work_bytes", "hxt_product_grad_work_bytes",
     "hxt_strerror", "hxt_last_hip_error", "hxt_version",
 )
 
@@ -40,6 +42,7 @@ _DTYPE_BY_TORCH = {
     torch.uint8: HXT_U8, torch.int8: HXT_U8, torch.bool: HXT_U8,
     torch.float16: HXT_F16, torch.int16: HXT_F16, torch.bfloat16: HXT_BF16,
     torch.float32: HXT_F32, torch.int32: HXT_F32, torch.float64: HXT_F64, torch.int64: HXT_F64,
+    torch.float8_e4m3fn: HXT_U8,                         # moved as bytes
 }
 _DTYPE_BY_SIZE = {1: HXT_U8, 2: HXT_BF16, 4: HXT_F32, 8: HXT_F64}
 
@@ -72,6 +75,37 @@ class _Exchange(C.Structure):
                 ("tags_send", C.POINTER(C.c_void_p)), ("tags_recv", C.POINTER(C.c_void_p)),
                 ("tags_pinned", C.POINTER(C.c_void_p)), ("status", C.c_void_p), ("seq_base", C.c_uint64),
                 ("direct_mode", C.c_int), ("drain_every", C.c_int)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int), ("eps", C.c_float),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("residual", C.c_void_p), ("residual_stride", C.c_int64),
+                ("weight", C.c_void_p), ("h", C.c_void_p), ("h_stride", C.c_int64), ("y", C.c_void_p), ("y_stride", C.c_int64),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("scale", C.c_void_p)]
+
+
+class _NormGrad(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int), ("eps", C.c_float),
+                ("h", C.c_void_p), ("h_stride", C.c_int64), ("dy", C.c_void_p), ("dy_stride", C.c_int64),
+                ("dh", C.c_void_p), ("dh_stride", C.c_int64), ("weight", C.c_void_p), ("dx", C.c_void_p), ("dx_stride", C.c_int64),
+                ("dweight", C.c_void_p), ("dweight_add", C.c_void_p), ("work", C.c_void_p), ("work_bytes", C.c_size_t)]
+
+
+class _Product(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("dtype", C.c_int), ("out_dtype", C.c_int), ("act", C.c_int),
+                ("a", C.c_void_p), ("a_stride", C.c_int64), ("b", C.c_void_p), ("b_stride", C.c_int64),
+                ("a_scale", C.c_void_p), ("b_scale", C.c_void_p), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("residual_stride", C.c_int64), ("pre", C.c_void_p), ("pre_stride", C.c_int64),
+                ("c", C.c_void_p), ("c_stride", C.c_int64), ("work", C.c_void_p), ("work_bytes", C.c_size_t)]
+
+
+class _ProductGrad(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("db_dtype", C.c_int), ("act", C.c_int),
+                ("dc", C.c_void_p), ("dc_stride", C.c_int64), ("pre", C.c_void_p), ("pre_stride", C.c_int64),
+                ("a", C.c_void_p), ("a_stride", C.c_int64), ("b", C.c_void_p), ("b_stride", C.c_int64),
+                ("dz", C.c_void_p), ("dz_stride", C.c_int64), ("da", C.c_void_p), ("da_stride", C.c_int64),
+                ("db", C.c_void_p), ("db_stride", C.c_int64), ("db_add", C.c_void_p), ("db_add_stride", C.c_int64),
+                ("dbias", C.c_void_p), ("dbias_add", C.c_void_p), ("work", C.c_void_p), ("work_bytes", C.c_size_t)]
 
 
 HXT_DEVICE_DIRECT, HXT_CPU_FORWARD = 0, 1
@@ -135,6 +169,16 @@ def lib():
             "hxt_unpack_verify_batch": (i, [i, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(C.c_uint64),
                                             C.POINTER(C.c_uint32), C.POINTER(C.POINTER(vp)), C.POINTER(vp), vp]),
             "hxt_pack_noalloc": (i, [vp, sz, i, sz, vp, u64p, vp]),
+            "hxt_norm": (i, [C.POINTER(_Norm), vp]),
+            "hxt_unpack_norm": (i, [vp, vp, C.POINTER(_Norm), u64p, vp]),
+            "hxt_norm_grad_work_bytes": (sz, [C.c_int64, C.c_int64]),
+            "hxt_norm_grad": (i, [C.POINTER(_NormGrad), vp]),
+            "hxt_pack_norm_grad": (i, [vp, C.POINTER(_NormGrad), vp, u64p, vp]),
+            "hxt_product_work_bytes": (sz, [C.c_int64, C.c_int64, C.c_int64, i]),
+            "hxt_product": (i, [C.POINTER(_Product), vp]),
+            "hxt_pack_product": (i, [vp, C.POINTER(_Product), vp, u64p, vp]),
+            "hxt_product_grad_work_bytes": (sz, [C.c_int64, C.c_int64, C.c_int64]),
+            "hxt_product_grad": (i, [C.POINTER(_ProductGrad), vp]),
             "hxt_strerror": (C.c_char_p, [i]),
             "hxt_last_hip_error": (i, []),
             "hxt_version": (C.c_char_p, []),
@@ -463,6 +507,209 @@ def hxt_stage_d2h_slots(plan: Plan, lane: int, first_slot: int, n_slots: int, pa
 def hxt_stage_h2d_slots(plan: Plan, lane: int, first_slot: int, n_slots: int, host_pinned, packed_dev, stream=None) -> None:
     _check(lib().hxt_stage_h2d_slots(plan.handle, lane, first_slot, n_slots, _ptr(host_pinned), _ptr(packed_dev),
                                      _stream(stream)), "hxt_stage_h2d_slots")
+
+
+# ---- operators at the ends of a stage -----------------------------------------------------------
+
+HXT_ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+_NUMBERS = {torch.bfloat16: HXT_BF16, torch.float32: HXT_F32}
+_FACTORS = {torch.bfloat16: HXT_BF16, torch.float8_e4m3fn: HXT_E4M3}
+
+
+class _Arguments:
+    """Marshals tensors into one of the argument blocks, with the checks that pointers alone do not allow."""
+
+    def __init__(self, block):
+        self.c = block
+        self.device = None
+        self._keep = []
+
+    def _own(self, name, t):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s: a tensor is expected" % name)
+        if self.device is None:
+            self.device = t.device
+        elif t.device != self.device:
+            raise ValueError("%s is on %s, other arguments on %s" % (name, t.device, self.device))
+        self._keep.append(t)
+        setattr(self.c, name, t.data_ptr())
+
+    def matrix(self, name, t, rows, cols, dtype):
+        """A [..., cols] tensor whose leading dimensions are evenly spaced rows."""
+        if t is None:
+            return
+        if t.dtype != dtype:
+            raise ValueError("%s is %s, not %s" % (name, t.dtype, dtype))
+        v = t if t.dim() == 2 else t.reshape(1, 1) if t.dim() == 0 else t.unsqueeze(0) if t.dim() == 1 else t.view(-1, t.shape[-1])
+        if tuple(v.shape) != (rows, cols):
+            raise ValueError("%s is %s, not rows of [%d, %d]" % (name, tuple(t.shape), rows, cols))
+        if cols > 1 and v.stride(1) != 1 and v.numel():
+            raise ValueError("%s: the elements of a row must be adjacent" % name)
+        self._own(name, t)
+        setattr(self.c, name + "_stride", v.stride(0))
+
+    def vector(self, name, t, n, dtype):
+        if t is None:
+            return
+        if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+            raise ValueError("%s must be %d adjacent elements of %s" % (name, n, dtype))
+        self._own(name, t)
+
+    def workspace(self, t):
+        if t is None:
+            return
+        if not t.is_contiguous():
+            raise ValueError("work must be contiguous")
+        self._own("work", t)
+        self.c.work_bytes = t.numel() * t.element_size()
+
+    def pointer(self):
+        """The block's address for a call made now: its tensors must be on the GPU that is current."""
+        d = self.device
+        if d.type == "cuda" and d.index != torch._C._cuda_getDevice():
+            raise ValueError("the arguments are on %s, the current device is cuda:%d" % (d, torch._C._cuda_getDevice()))
+        if d.type != "cuda" and torch.cuda.is_available():
+            raise ValueError("the arguments are on %s" % d)
+        return C.byref(self.c)
+
+
+def _shape_of(named):
+    for t in named:
+        if t is not None:
+            cols = t.shape[-1] if t.dim() else 1
+            return (t.numel() // cols if cols else (t.shape[0] if t.dim() == 2 else 0)), cols
+    raise ValueError("no tensor says how many rows there are")
+
+
+def _type(table, t, what):
+    if t not in table:
+        raise ValueError("%s: %s is not supported" % (what, t))
+    return table[t]
+
+
+def _message_of_numbers(plan: Plan, where: str) -> None:
+    if not plan.arithmetic:
+        raise ValueError("%s computes with bf16 or f32 values: build the plan with torch.bfloat16 / torch.float32" % where)
+
+
+class Norm(_Arguments):
+    """Arguments of hxt_norm and (x left out) of hxt_unpack_norm.  The tensors must outlive the calls; the block may be used
+    for any number of them."""
+
+    def __init__(self, weight=None, eps: float = 1e-5, x=None, residual=None, h=None, y=None, q=None, scale=None):
+        super().__init__(_Norm())
+        rows, cols = _shape_of([x, h, y, q])
+        dt = next((t.dtype for t in (x, residual, h, y, weight) if t is not None), None)
+        if dt is None:
+            raise ValueError("give weight, h or y: nothing says what type the rows have")
+        self.c.rows, self.c.cols, self.c.dtype, self.c.eps = rows, cols, _type(_NUMBERS, dt, "rows"), eps
+        for name, t in (("x", x), ("residual", residual), ("h", h), ("y", y)):
+            self.matrix(name, t, rows, cols, dt)
+        self.vector("weight", weight, cols, dt)
+        self.matrix("q", q, rows, cols, torch.float8_e4m3fn)
+        self.vector("scale", scale, rows, torch.float32)
+
+
+def hxt_norm(a: Norm, stream=None) -> None:
+    _check(lib().hxt_norm(a.pointer(), _stream(stream)), "hxt_norm")
+
+
+def hxt_unpack_norm(plan: Plan, packed, a: Norm, sums=None, stream=None) -> None:
+    _message_of_numbers(plan, "hxt_unpack_norm")
+    _check(lib().hxt_unpack_norm(plan.handle, _ptr(packed), a.pointer(), _ptr(sums), _stream(stream)), "hxt_unpack_norm")
+
+
+def hxt_norm_grad_work_bytes(rows: int, cols: int) -> int:
+    return lib().hxt_norm_grad_work_bytes(rows, cols)
+
+
+class NormGrad(_Arguments):
+    """Arguments of hxt_norm_grad and (dx left out) of hxt_pack_norm_grad."""
+
+    def __init__(self, weight=None, eps: float = 1e-5, h=None, dy=None, dh=None, dx=None, dweight=None, dweight_add=None, work=None):
+        super().__init__(_NormGrad())
+        rows, cols = _shape_of([h, dy])
+        dt = next(t.dtype for t in (h, dy) if t is not None)
+        self.c.rows, self.c.cols, self.c.dtype, self.c.eps = rows, cols, _type(_NUMBERS, dt, "rows"), eps
+        for name, t in (("h", h), ("dy", dy), ("dh", dh), ("dx", dx)):
+            self.matrix(name, t, rows, cols, dt)
+        self.vector("weight", weight, cols, dt)
+        self.vector("dweight", dweight, cols, torch.float32)
+        self.vector("dweight_add", dweight_add, cols, torch.float32)
+        self.workspace(work)
+
+
+def hxt_norm_grad(a: NormGrad, stream=None) -> None:
+    _check(lib().hxt_norm_grad(a.pointer(), _stream(stream)), "hxt_norm_grad")
+
+
+def hxt_pack_norm_grad(plan: Plan, a: NormGrad, packed, sums=None, stream=None) -> None:
+    _message_of_numbers(plan, "hxt_pack_norm_grad")
+    _check(lib().hxt_pack_norm_grad(plan.handle, a.pointer(), _ptr(packed), _ptr(sums), _stream(stream)), "hxt_pack_norm_grad")
+
+
+def hxt_product_work_bytes(m: int, n: int, k: int, dtype=torch.bfloat16) -> int:
+    return lib().hxt_product_work_bytes(m, n, k, _type(_FACTORS, dtype, "factors"))
+
+
+class Product(_Arguments):
+    """Arguments of hxt_product and (c left out) of hxt_pack_product: a [m, k] times the rows of b [n, k]."""
+
+    def __init__(self, a, b, a_scale=None, b_scale=None, bias=None, act: str = "none", residual=None, pre=None, c=None, work=None,
+                 out_dtype=torch.bfloat16):
+        super().__init__(_Product())
+        (m, k), (n, kb) = _shape_of([a]), _shape_of([b])
+        if k != kb:
+            raise ValueError("a has rows of %d, b of %d" % (k, kb))
+        blk = self.c
+        blk.m, blk.n, blk.k = m, n, k
+        blk.dtype, blk.out_dtype, blk.act = _type(_FACTORS, a.dtype, "factors"), _type(_NUMBERS, out_dtype, "out_dtype"), _type(HXT_ACT, act, "act")
+        self.matrix("a", a, m, k, a.dtype)
+        self.matrix("b", b, n, k, a.dtype)
+        self.vector("a_scale", a_scale, m, torch.float32)
+        self.vector("b_scale", b_scale, n, torch.float32)
+        self.vector("bias", bias, n, torch.bfloat16)
+        self.matrix("residual", residual, m, n, out_dtype)
+        self.matrix("pre", pre, m, n, torch.bfloat16)
+        self.matrix("c", c, m, n, out_dtype)
+        self.workspace(work)
+
+
+def hxt_product(a: Product, stream=None) -> None:
+    _check(lib().hxt_product(a.pointer(), _stream(stream)), "hxt_product")
+
+
+def hxt_pack_product(plan: Plan, a: Product, packed, sums=None, stream=None) -> None:
+    _message_of_numbers(plan, "hxt_pack_product")
+    _check(lib().hxt_pack_product(plan.handle, a.pointer(), _ptr(packed), _ptr(sums), _stream(stream)), "hxt_pack_product")
+
+
+def hxt_product_grad_work_bytes(m: int, n: int, k: int) -> int:
+    return lib().hxt_product_grad_work_bytes(m, n, k)
+
+
+class ProductGrad(_Arguments):
+    """Arguments of hxt_product_grad."""
+
+    def __init__(self, dc, a=None, b=None, pre=None, act: str = "none", dz=None, da=None, db=None, dbias=None, db_add=None,
+                 dbias_add=None, work=None):
+        super().__init__(_ProductGrad())
+        m, n = _shape_of([dc])
+        k = next((t.shape[-1] for t in (a, b, da, db) if t is not None), 0)
+        blk, bf16 = self.c, torch.bfloat16
+        db_dtype = db.dtype if db is not None else bf16
+        blk.m, blk.n, blk.k, blk.db_dtype, blk.act = m, n, k, _type(_NUMBERS, db_dtype, "db"), _type(HXT_ACT, act, "act")
+        for name, t, rows, cols, dt in (("dc", dc, m, n, bf16), ("pre", pre, m, n, bf16), ("a", a, m, k, bf16), ("b", b, n, k, bf16),
+                                        ("dz", dz, m, n, bf16), ("da", da, m, k, bf16), ("db", db, n, k, db_dtype),
+                                        ("db_add", db_add, n, k, db_dtype)):
+            self.matrix(name, t, rows, cols, dt)
+        self.vector("dbias", dbias, n, torch.float32)
+        self.vector("dbias_add", dbias_add, n, torch.float32)
+        self.workspace(work)
+
+
+def hxt_product_grad(a: ProductGrad, stream=None) -> None:
+    _check(lib().hxt_product_grad(a.pointer(), _stream(stream)), "hxt_product_grad")
 
 
 def hxt_version() -> str:

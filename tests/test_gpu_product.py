@@ -1,0 +1,333 @@
+"""hxt_product, hxt_pack_product and hxt_product_grad against their formulas in 64 bits.
+
+Products of small whole numbers are exact in binary32 whatever their order, so those must agree to the last bit (bf16 results: the exact
+value rounded once).  For other values a sum of k terms may be off by k * 2^-24 of the sum of their magnitudes (any order), an
+activation by 2^-16 of its value and by 1.2 times its argument's error (the steepest slope is gelu's 1.13).  The matrix instruction for
+8-bit factors lines its 128 products up with the largest one and keeps 20 bits below it: 128 * 2^-20 of the largest magnitude, so
+2^-13 of their sum (its results are bf16 only, 2^-8)."""
+import pytest
+import torch
+
+from paper_2602_18007_amd import hxt
+from tests.operator_cases import BF16, DEV, E4M3, F32, HALF, Guarded, act_exact, act_grad_exact, f64, generator, normal, within
+
+pytestmark = pytest.mark.gpu
+
+
+def whole(shape, g, most=4):
+    return torch.randint(-most, most + 1, shape, generator=g, device=DEV).to(F32)
+
+
+def workspace(m, n, k, dtype=BF16):
+    return Guarded(1, hxt.hxt_product_work_bytes(m, n, k, dtype), torch.uint8)
+
+
+def exact(a, b, a_scale=None, b_scale=None, bias=None, act="none", residual=None):
+    z, size = f64(a) @ f64(b).t().contiguous(), f64(a).abs() @ f64(b).abs().t().contiguous()
+    if a_scale is not None:
+        z, size = z * f64(a_scale)[:, None], size * f64(a_scale)[:, None]
+    if b_scale is not None:
+        z, size = z * f64(b_scale), size * f64(b_scale)
+    if bias is not None:
+        z = z + f64(bias)
+    c = act_exact(z, act)
+    return z, (c if residual is None else c + f64(residual)), size
+
+
+SIZES = [(1, 1, 1), (1, 16, 8), (3, 5, 7), (1, 256, 1000), (2, 17, 64), (16, 64, 128), (17, 130, 65), (61, 200, 96), (64, 129, 512), (127, 128, 72),
+         (128, 127, 1), (129, 257, 136), (255, 64, 130), (256, 256, 64), (257, 520, 192), (300, 1000, 1023), (1, 4096, 4096), (16, 1024, 2048), (33, 96, 2056)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_products_of_whole_numbers_are_exact(m, n, k, dtype):
+    """Aligned and odd bases and pitches, both output types; nothing beside the outputs is written."""
+    print("product", m, n, k, dtype, flush=True)
+    g = generator(m * 31 + n * 17 + k)
+    for pad, offset in ((0, 0), (16, 0), (1, 1), (5, 3)):
+        a = Guarded(m, k, dtype, pad, offset).set(whole((m, k), g))
+        b = Guarded(n, k, dtype, pad, offset).set(whole((n, k), g))
+        z = f64(a.m) @ f64(b.m).t().contiguous()
+        for out in (F32, BF16) if dtype == BF16 else (BF16,):
+            c, work = Guarded(m, n, out, pad, offset), workspace(m, n, k, dtype)
+            hxt.hxt_product(hxt.Product(a.m, b.m, c=c.m, out_dtype=out, work=work.m.view(-1)))
+            assert torch.equal(c.m, z.to(F32).to(out)), "%s: %d differ" % ((pad, offset, out), int((c.m != z.to(F32).to(out)).sum()))
+            assert c.untouched() and work.untouched()
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("m,n,k", [(1, 40, 72), (5, 33, 17), (64, 96, 256), (130, 136, 200), (1, 256, 4096), (257, 264, 320)])
+def test_product_with_its_epilogue(m, n, k, act):
+    g = generator(m + n + k)
+    for dtype in (BF16, E4M3):
+        a, b = normal((m, k), g, 1.0, dtype), normal((n, k), g, k ** -0.5, dtype)
+        sa, sb = (torch.rand(m, generator=g, device=DEV) + 0.5, torch.rand(n, generator=g, device=DEV) + 0.5) if dtype == E4M3 else (None, None)
+        bias = normal((n,), g, 1.0, BF16)
+        for out, pad in ((BF16, 0), (F32 if dtype == BF16 else BF16, 3)):
+            residual = Guarded(m, n, out, pad).set(normal((m, n), g, 2.0))
+            pre, c, work = Guarded(m, n, BF16, pad), Guarded(m, n, out, pad), workspace(m, n, k, dtype)
+            hxt.hxt_product(hxt.Product(a, b, a_scale=sa, b_scale=sb, bias=bias, act=act, residual=residual.m, pre=pre.m, c=c.m, out_dtype=out,
+                                        work=work.m.view(-1)))
+            Z, C, size = exact(a, b, sa, sb, bias, act, residual.m)
+            z_err = size * ((k + 4) * 2.0 ** -24 + (2.0 ** -13 if dtype == E4M3 else 0)) + Z.abs() * 2.0 ** -22 + 2.0 ** -22
+            within(pre.m, Z, z_err + Z.abs() * HALF[BF16], "pre")
+            c_err = 1.2 * z_err + act_exact(Z, act).abs() * 2.0 ** -16
+            within(c.m, C, c_err * (1 + HALF[out]) + C.abs() * (HALF[out] + 2.0 ** -24), "c")
+            assert pre.untouched() and c.untouched()
+            # the same into the residual's own matrix, without the rest
+            if act == "none":
+                C = exact(a, b, residual=residual.m)[1]
+                hxt.hxt_product(hxt.Product(a, b, residual=residual.m, c=residual.m, out_dtype=out, work=work.m.view(-1)))
+                plain_err = exact(a, b)[2] * ((k + 4) * 2.0 ** -24 + (2.0 ** -13 if dtype == E4M3 else 0))
+                within(residual.m, C, plain_err * (1 + HALF[out]) + C.abs() * (HALF[out] + 2.0 ** -23), "c over its residual")
+                assert residual.untouched()
+
+
+def test_product_scales_alone_and_broadcast_rows():
+    g = generator(5)
+    m, n, k = 70, 90, 160
+    a, b = whole((m, k), g).to(E4M3), whole((n, k), g).to(E4M3)
+    sa, sb = 2.0 ** torch.randint(-3, 4, (m,), generator=g, device=DEV).float(), 2.0 ** torch.randint(-3, 4, (n,), generator=g, device=DEV).float()
+    for x, y in ((sa, None), (None, sb), (sa, sb), (None, None)):
+        c = torch.empty(m, n, dtype=BF16, device=DEV)
+        hxt.hxt_product(hxt.Product(a, b, a_scale=x, b_scale=y, c=c, work=workspace(m, n, k, E4M3).m.view(-1)))
+        assert torch.equal(c, exact(a, b, x, y)[0].to(F32).to(BF16))
+    one = whole((1, k), g).to(BF16)
+    wide = one.expand(m, k)
+    c, w = torch.empty(m, n, device=DEV), whole((n, k), g).to(BF16)
+    hxt.hxt_product(hxt.Product(wide, w, residual=c[:1].zero_().expand(m, n).contiguous(), c=c, out_dtype=F32, work=workspace(m, n, k).m.view(-1)))
+    assert torch.equal(c, exact(wide, w)[0].to(F32))
+    r = whole((1, n), g)
+    hxt.hxt_product(hxt.Product(wide, w, residual=r.expand(m, n), c=c, out_dtype=F32, work=workspace(m, n, k).m.view(-1)))
+    assert torch.equal(c, (exact(wide, w)[0] + f64(r)).to(F32))
+
+
+def test_product_of_an_empty_sum():
+    m, n = 20, 30
+    g = generator(6)
+    bias, r = normal((n,), g, 1.0, BF16), normal((m, n), g, 1.0, BF16)
+    c, pre = torch.empty(m, n, dtype=BF16, device=DEV), torch.empty(m, n, dtype=BF16, device=DEV)
+    hxt.hxt_product(hxt.Product(torch.empty(m, 0, dtype=BF16, device=DEV), torch.empty(n, 0, dtype=BF16, device=DEV), bias=bias, act="relu", residual=r, pre=pre, c=c))
+    assert torch.equal(pre, bias.expand(m, n))
+    want = torch.relu(f64(bias)) + f64(r)
+    within(c, want, want.abs() * HALF[BF16], "c")
+
+
+def test_what_is_not_finite_stays_in_its_row_and_column():
+    """NaN and infinities in padded places behind a row, and in rows past the matrix, do not enter; in the matrix they reach their row
+    and column alone."""
+    g = generator(7)
+    for dtype, m, n, k in ((BF16, 40, 50, 77), (BF16, 3, 33, 40), (E4M3, 40, 50, 77), (BF16, 140, 136, 72)):
+        big_a = torch.full((m + 3, k + 9), float("nan"), device=DEV).to(dtype)
+        big_b = torch.full((n + 3, k + 9), float("nan"), device=DEV).to(dtype)
+        a, b = big_a[:m, :k], big_b[:n, :k]
+        a.copy_(whole((m, k), g).to(dtype))
+        b.copy_(whole((n, k), g).to(dtype))
+        out = F32 if dtype == BF16 else BF16
+        c, work = torch.empty(m, n, dtype=out, device=DEV), workspace(m, n, k, dtype).m.view(-1)
+        hxt.hxt_product(hxt.Product(a, b, c=c, out_dtype=out, work=work))
+        assert torch.equal(c, exact(a, b)[0].to(F32).to(out))
+        a[1, 5] = float("nan")
+        b[2, k - 1] = float("nan")
+        hxt.hxt_product(hxt.Product(a, b, c=c, out_dtype=out, work=work))
+        bad = torch.zeros(m, n, dtype=torch.bool, device=DEV)
+        bad[1], bad[:, 2] = True, True
+        assert torch.equal(torch.isnan(c), bad)
+
+
+@pytest.mark.parametrize("m,n,k,lanes,chunk", [(1, 4096, 512, 2, 2048), (7, 33, 40, 3, 256), (130, 264, 96, 4, 8192), (64, 1001, 200, 2, 768),
+                                               (300, 520, 64, 8, 65536), (16, 128, 8192, 2, 256), (257, 257, 33, 2, 1 << 20)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_product_into_a_message(m, n, k, lanes, chunk, out):
+    print("pack product", m, n, k, lanes, chunk, out, flush=True)
+    g = generator(m + n)
+    a, b, r = whole((m, k), g).to(BF16), whole((n, k), g).to(BF16), whole((m, n), g).to(out)
+    plan = hxt.hxt_plan((m, 1, n), None, out, lanes, chunk)
+    want = torch.full((plan.packed_bytes,), 0xA5, dtype=torch.uint8, device=DEV)
+    want_sums = torch.empty(plan.num_chunks, dtype=torch.int64, device=DEV)
+    hxt.hxt_pack(plan, [(exact(a, b)[0] + f64(r)).to(F32).to(out)], want, want_sums)
+    call = hxt.Product(a, b, residual=r, out_dtype=out, work=workspace(m, n, k).m.view(-1))
+    for sums in (None, torch.full_like(want_sums, -1), torch.full_like(want_sums, -1)):
+        packed = torch.full_like(want, 0xA5)
+        hxt.hxt_pack_product(plan, call, packed, sums)
+        assert torch.equal(packed, want)
+        assert sums is None or torch.equal(sums, want_sums)
+
+
+GRADS = [(1, 1, 1), (1, 64, 8), (5, 7, 3), (17, 130, 65), (64, 128, 256), (129, 136, 72), (200, 264, 520), (300, 1000, 96), (1021, 100, 51), (2100, 16, 24)]
+
+
+@pytest.mark.parametrize("m,n,k", GRADS)
+def test_product_grad_of_whole_numbers_is_exact(m, n, k):
+    print("product grad", m, n, k, flush=True)
+    g = generator(m * 5 + n * 3 + k)
+    for pad, offset in ((0, 0), (8, 0), (3, 1)):
+        dc = Guarded(m, n, BF16, pad, offset).set(whole((m, n), g))
+        a = Guarded(m, k, BF16, pad, offset).set(whole((m, k), g))
+        b = Guarded(n, k, BF16, pad, offset).set(whole((n, k), g))
+        da, dbias = Guarded(m, k, BF16, pad, offset), Guarded(1, n, F32)
+        work = Guarded(1, hxt.hxt_product_grad_work_bytes(m, n, k), torch.uint8)
+        for out in (F32, BF16):
+            db = Guarded(n, k, out, pad, offset)
+            hxt.hxt_product_grad(hxt.ProductGrad(dc.m, a.m, b.m, da=da.m, db=db.m, dbias=dbias.m.view(-1), work=work.m.view(-1)))
+            assert torch.equal(da.m, (f64(dc.m) @ f64(b.m)).to(F32).to(BF16)), "da"
+            assert torch.equal(db.m, (f64(dc.m).t().contiguous() @ f64(a.m)).to(F32).to(out)), "db"
+            assert torch.equal(dbias.m.view(-1), f64(dc.m).sum(0).to(F32)), "dbias"
+            assert da.untouched() and db.untouched() and dbias.untouched() and work.untouched()
+            add, badd = whole((n, k), g).to(out), whole((n,), g)
+            into = add.clone()
+            hxt.hxt_product_grad(hxt.ProductGrad(dc.m, a.m, db=into, db_add=into, dbias=dbias.m.view(-1), dbias_add=badd, work=work.m.view(-1)))
+            assert torch.equal(into, (f64(dc.m).t().contiguous() @ f64(a.m) + f64(add)).to(F32).to(out)), "db added"
+            assert torch.equal(dbias.m.view(-1), (f64(dc.m).sum(0) + f64(badd)).to(F32))
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("m,n,k", [(1, 16, 24), (37, 65, 33), (256, 264, 128), (700, 520, 72)])
+def test_product_grad_through_an_activation(m, n, k, act):
+    g = generator(m + n * k)
+    dc, pre, a, b = normal((m, n), g, 0.1, BF16), normal((m, n), g, 2.0, BF16), normal((m, k), g, 1.0, BF16), normal((n, k), g, k ** -0.5, BF16)
+    dz, da, db, dbias = torch.empty_like(dc), torch.empty_like(a), torch.empty_like(b), torch.empty(n, device=DEV)
+    work = torch.empty(hxt.hxt_product_grad_work_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(dc, a, b, pre=pre, act=act, dz=dz, da=da, db=db, dbias=dbias, work=work))
+    D = f64(dc) * act_grad_exact(f64(pre), act)
+    # the derivative is a sum of terms up to a few times its steepest value (1.13): 2^-16 each
+    err = f64(dc).abs() * 4 * 2.0 ** -16
+    within(dz, D, err + D.abs() * (HALF[BF16] + 2.0 ** -16), "dz")
+    within(dbias, D.sum(0), err.sum(0) + D.abs().sum(0) * m * 2.0 ** -24, "dbias")
+    Z = f64(dz)                                          # what the products read
+    for got, x, y, depth, what in ((da, Z, f64(b), n, "da"), (db, Z.t().contiguous(), f64(a), m, "db")):
+        want, size = x @ y, x.abs() @ y.abs()
+        within(got, want, size * (depth + 4) * 2.0 ** -24 + want.abs() * (HALF[BF16] + 2.0 ** -24) + 2.0 ** -134, what)
+    into = dc.clone()                                    # the gradient in its own place
+    hxt.hxt_product_grad(hxt.ProductGrad(into, pre=pre, act=act, dz=into, work=work))
+    assert torch.equal(into, dz)
+
+
+def test_product_grad_against_differences():
+    """Central differences of the 64-bit product: bf16 gradients are within their rounding (and dz's, which enters them)."""
+    g = generator(9)
+    m, n, k = 4, 6, 5
+    a, b, c = normal((m, k), g, 1.0, BF16), normal((n, k), g, 1.0, BF16), normal((m, n), g, 1.0, BF16)
+    bias = normal((n,), g, 1.0, BF16)
+    pre, out = torch.empty(m, n, dtype=BF16, device=DEV), torch.empty(m, n, dtype=BF16, device=DEV)
+    hxt.hxt_product(hxt.Product(a, b, bias=bias, act="gelu", pre=pre, c=out))
+    dz, da, db, dbias = torch.empty_like(c), torch.empty_like(a), torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+    work = torch.empty(hxt.hxt_product_grad_work_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(c, a, b, pre=pre, act="gelu", dz=dz, da=da, db=db, dbias=dbias, work=work))
+    ts = [f64(a), f64(b), f64(bias)]
+    loss = lambda: (act_exact(ts[0] @ ts[1].t().contiguous() + ts[2], "gelu") * f64(c)).sum().item()       # noqa: E731
+    for t, got in zip(ts, (da, db, dbias)):
+        flat = t.view(-1)
+        for i in range(flat.numel()):
+            keep, step = flat[i].item(), 1e-5
+            flat[i] = keep + step
+            up = loss()
+            flat[i] = keep - step
+            down = loss()
+            flat[i] = keep
+            # pre is rounded to bf16 (|pre| < 16: off by 2^-5 at most, and the derivative's slope is below 1.2), dz to bf16: with
+            # at most 6 terms of magnitude below 4 * 4 each
+            assert abs((up - down) / (2 * step) - got.view(-1)[i].item()) < 6 * 16 * (2.0 ** -5 * 1.2 + 2.0 ** -8)
+
+
+def test_product_grad_of_nothing():
+    m, n, k = 0, 8, 16
+    e = torch.empty(0, 8, dtype=BF16, device=DEV)
+    add, badd = normal((n, k), generator(1)), normal((n,), generator(2))
+    db, dbias = torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(e, torch.empty(0, k, dtype=BF16, device=DEV), db=db, db_add=add, dbias=dbias, dbias_add=badd))
+    assert torch.equal(db, add) and torch.equal(dbias, badd)
+    a, b = torch.empty(5, k, dtype=BF16, device=DEV), torch.empty(0, k, dtype=BF16, device=DEV)
+    da = torch.full((5, k), 3.0, dtype=BF16, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(torch.empty(5, 0, dtype=BF16, device=DEV), a, b, da=da))
+    assert bool((da == 0).all())
+
+
+def test_a_stage_from_message_to_message():
+    """The operators together: a message with its residual is received, normed into 8 bits, multiplied, activated, multiplied back with the
+    residual in the epilogue and sent; the gradient's message comes back the other way.  Forward and backward are captured into
+    one graph and replayed on new messages."""
+    rows, hidden, inner = 96, 512, 1280
+    g = generator(20)
+    w = (1 + 0.2 * normal((hidden,), g)).to(BF16)
+    up, down = normal((inner, hidden), g, hidden ** -0.5, BF16), normal((hidden, inner), g, inner ** -0.5, BF16)
+    up_scale = f64(up).abs().amax(1).float() / 448.0
+    up8 = (up.float() / up_scale[:, None]).to(E4M3)
+    bias = normal((inner,), g, 0.1, BF16)
+    two, one = hxt.hxt_plan_multi([((rows, hidden), None, BF16)] * 2, 4, 8192), hxt.hxt_plan((rows, hidden), None, BF16, 4, 8192)
+    box = lambda p: torch.zeros(p.packed_bytes, dtype=torch.uint8, device=DEV)                              # noqa: E731
+    sums = lambda p: torch.zeros(p.num_chunks, dtype=torch.int64, device=DEV)                               # noqa: E731
+    new = lambda r, c, t=BF16: torch.empty(r, c, dtype=t, device=DEV)                                       # noqa: E731
+    arrived, sent, grad_in, grad_out = box(two), box(one), box(one), box(one)
+    s_in, s_out, s_gin, s_gout = sums(two), sums(one), sums(one), sums(one)
+    h, q, y, scale = new(rows, hidden), new(rows, hidden, E4M3), new(rows, hidden), torch.empty(rows, device=DEV)
+    z, mid, out_grad, dmid, dz, dy = new(rows, inner), new(rows, inner), new(rows, hidden), new(rows, inner), new(rows, inner), new(rows, hidden)
+    dup, ddown, dbias, dw = new(inner, hidden, F32), new(hidden, inner, F32), torch.empty(inner, device=DEV), torch.empty(hidden, device=DEV)
+    work = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (
+        hxt.hxt_product_work_bytes(rows, inner, hidden, E4M3), hxt.hxt_product_work_bytes(rows, hidden, inner),
+        hxt.hxt_product_grad_work_bytes(rows, hidden, inner), hxt.hxt_product_grad_work_bytes(rows, inner, hidden), hxt.hxt_norm_grad_work_bytes(rows, hidden))]
+    norm = hxt.Norm(w, 1e-5, h=h, q=q, y=y, scale=scale)
+    first = hxt.Product(q, up8, a_scale=scale, b_scale=up_scale, bias=bias, act="silu", pre=z, c=mid, work=work[0])
+    second = hxt.Product(mid, down, residual=h, work=work[1])
+    second_grad = hxt.ProductGrad(out_grad, mid, down, da=dmid, db=ddown, work=work[2])
+    first_grad = hxt.ProductGrad(dmid, y, up, pre=z, act="silu", dz=dz, da=dy, db=dup, dbias=dbias, work=work[3])
+    norm_grad = hxt.NormGrad(w, 1e-5, h=h, dy=dy, dh=out_grad, dweight=dw, work=work[4])
+
+    def step(st):
+        hxt.hxt_unpack_norm(two, arrived, norm, s_in, st)
+        hxt.hxt_product(first, st)
+        hxt.hxt_pack_product(one, second, sent, s_out, st)
+        hxt.hxt_unpack(one, grad_in, [out_grad], s_gin, st)
+        hxt.hxt_product_grad(second_grad, st)
+        hxt.hxt_product_grad(first_grad, st)
+        hxt.hxt_pack_norm_grad(one, norm_grad, grad_out, s_gout, st)
+
+    def check(x, r, dout):
+        X, R, W = f64(x), f64(r), f64(w)
+        H = X + R
+        N = H / torch.sqrt((H * H).mean(1, keepdim=True) + 1e-5)
+        Z = (N * W) @ f64(up).t().contiguous() + f64(bias)
+        M = act_exact(Z, "silu")
+        OUT = M @ f64(down).t().contiguous() + H
+        D = f64(dout)
+        DZ = (D @ f64(down)) * act_grad_exact(Z, "silu")
+        DY = DZ @ f64(up)
+        G = DY * W
+        rstd = 1 / torch.sqrt((H * H).mean(1, keepdim=True) + 1e-5)
+        DX = rstd * (G - N * (G * N).mean(1, keepdim=True)) + D
+        got_out, got_dx, got_sums = torch.empty_like(x), torch.empty_like(x), sums(one)
+        hxt.hxt_unpack(one, sent, [got_out], got_sums)
+        assert torch.equal(got_sums, s_out)
+        hxt.hxt_unpack(one, grad_out, [got_dx], got_sums)
+        assert torch.equal(got_sums, s_gout)
+        hxt.hxt_checksum(two, arrived, got2 := sums(two))
+        assert torch.equal(got2, s_in)
+        # Two 8-bit factors, each within 2^-4 of its value; the errors of hundreds of terms are of either sign, so that their norm
+        # stays below sqrt(2) * 2^-4 of the norm of the product that they enter, and less behind the residual and the derivative.
+        limit = 2 ** 0.5 * 2.0 ** -4
+        for got, want, what in ((got_out, OUT, "out"), (got_dx, DX, "dx"), (ddown, D.t().contiguous() @ M, "ddown"),
+                                (dup, DZ.t().contiguous() @ (N * W), "dup"), (dbias, DZ.sum(0), "dbias"), (dw, (DY * N).sum(0), "dw")):
+            off = float((f64(got) - want).norm() / want.norm())
+            assert off < limit, "%s is %g off" % (what, off)
+
+    side = torch.cuda.Stream()
+    graph = None
+    for i in range(4):
+        x, r, dout = normal((rows, hidden), g, 1.0, BF16), normal((rows, hidden), g, 1.0, BF16), normal((rows, hidden), g, 0.1, BF16)
+        hxt.hxt_pack(two, [x, r], arrived)
+        hxt.hxt_pack(one, [dout], grad_in)
+        torch.cuda.synchronize()
+        if i == 0:
+            step(side)
+            side.synchronize()
+        else:
+            if graph is None:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=side):
+                    step(side)
+            for t in (sent, grad_out, h, q, mid, dz, dup, dw):
+                t.view(torch.uint8).zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+        check(x, r, dout)
