@@ -428,21 +428,32 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm_grad(NormGradArgs a)
             if ((i * G + t) * V + j < a.cols) to[(i * G + t) * V + j] = dw[i * V + j];
 }
 
-// Column sums of n rows of partial sums: 16 slices of the rows side by side for 16 columns, joined in order.
-__global__ __launch_bounds__(256) void k_norm_grad_weight(const float *__restrict__ partial, uint32_t n, uint32_t cols, const float *add, float *dweight)
+// Column sums of n rows of partial sums: 4 columns a thread, 16 threads a row, SLICES of the rows side by side, joined in
+// order.  Bound by the reading of the rows: 8 of them are in flight per thread.
+template <int SLICES>
+__global__ __launch_bounds__(16 * SLICES) void k_column_sums(const float *__restrict__ partial, uint32_t n, uint32_t cols, const float *add, float *to)
 {
-    __shared__ float part[16][17];
-    const uint32_t c = threadIdx.x & 15, slice = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-    float s = 0;
-    if (col < cols)
-        for (uint32_t r = slice; r < n; r += 16) s += partial[size_t(r) * cols + col];
-    part[slice][c] = s;
-    __syncthreads();
-    if (slice || col >= cols) return;
-    s = 0;
+    __shared__ float part[SLICES][64];
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    const uint32_t quad = threadIdx.x & 15, slice = threadIdx.x >> 4, col = blockIdx.x * 64 + quad * 4;
+    f32x4 s = {0, 0, 0, 0};
+    if (col + 4 <= cols) {
+#pragma unroll 8
+        for (uint32_t r = slice; r < n; r += SLICES) s += *reinterpret_cast<const f32x4_any *>(partial + size_t(r) * cols + col);
+    } else {
+        for (uint32_t r = slice; r < n; r += SLICES)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += part[k][c];
-    dweight[col] = add ? add[col] + s : s;
+            for (uint32_t i = 0; i < 4; ++i)
+                if (col + i < cols) s[i] += partial[size_t(r) * cols + col + i];
+    }
+    *reinterpret_cast<f32x4 *>(&part[slice][quad * 4]) = s;
+    __syncthreads();
+    const uint32_t c = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || c >= cols) return;
+    float sum = 0;
+#pragma unroll 8
+    for (int k = 0; k < SLICES; ++k) sum += part[k][threadIdx.x];
+    to[c] = add ? add[c] + sum : sum;
 }
 
 // ---- launches -----------------------------------------------------------------------------
@@ -638,14 +649,20 @@ int run_norm_grad(const hxt_norm_grad_t &a, const Plan *p, uint8_t *packed, hipS
                 else k_norm_grad<T, G, EPT, false><<<groups, G < 256 ? 256 : G, 0, st>>>(n);
             });
         });
-    if (a.dweight)
-        k_norm_grad_weight<<<uint32_t((a.cols + 15) / 16), 256, 0, st>>>(static_cast<const float *>(a.work), groups * uint32_t(rows_of(shape)),
-                                                                        uint32_t(a.cols), a.dweight_add, a.dweight);
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? HXT_OK : operator_fail(e);
+    if (e != hipSuccess) return operator_fail(e);
+    return a.dweight ? operator_column_sums(static_cast<const float *>(a.work), groups * uint32_t(rows_of(shape)), uint32_t(a.cols), a.dweight_add, a.dweight, st) : HXT_OK;
 }
 
 }  // namespace
+
+int hxt::operator_column_sums(const float *partial, uint32_t n, uint32_t cols, const float *add, float *to, hipStream_t st)
+{
+    if (n <= 64) k_column_sums<16><<<(cols + 63) / 64, 256, 0, st>>>(partial, n, cols, add, to);
+    else k_column_sums<64><<<(cols + 63) / 64, 1024, 0, st>>>(partial, n, cols, add, to);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HXT_OK : operator_fail(e);
+}
 
 extern "C" {
 

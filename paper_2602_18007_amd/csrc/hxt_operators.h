@@ -22,6 +22,9 @@ int operator_sums(const hxt_plan_t *plan, const void *packed, uint64_t *sums, bo
 // Calls enqueue(ctx, cx) while the accumulators of hxt_unpack are this call's.
 int operator_unpack_sums(const hxt_plan_t *plan, uint64_t *sums, hipStream_t st, void (*enqueue)(void *ctx, const SumCtx &cx), void *ctx);
 
+// to[c] = add[c] (nullptr: 0) + the sum over n rows of partial[.][c], in an order fixed by n (hxt_norm.hip).
+int operator_column_sums(const float *partial, uint32_t n, uint32_t cols, const float *add, float *to, hipStream_t st);
+
 // ---- argument checks (host) ----------------------------------------------------------
 // A matrix as the calls take it.
 struct Matrix {

@@ -18,36 +18,49 @@ int64_t element_size(hxt_dtype_t t) { return t == HXT_BF16 ? 2 : (t == HXT_F32 ?
 
 // ---- which kernel ---------------------------------------------------------------------------
 struct Shape {
-    uint32_t tm, tn, splits, split_steps;
-    bool direct;
+    uint32_t tile;                 // 16: k_product_rows, 64: k_product_ring, else k_product's
+    uint32_t splits, split_steps;
 };
 
 uint32_t up(uint64_t n, uint64_t to) { return uint32_t((n + to - 1) / to); }
 
-// Parts of the contraction: enough workgroups for every CU where the tiles alone do not fill the chip, each part at least 8
-// steps long so that its ramp is paid for.
-uint32_t splits_for(uint64_t tiles, uint32_t steps)
+// Which kernel, and in how many parts of the contraction: the least time by these measured costs in us.
+//   A step (128 bytes of the contraction) of a full round of workgroups, a round being what the chip holds at a time:
+//   256 x 256 tiles, one a CU, 1.5 (4096 x 4096 x 14336: 341 us in one round of 224 steps); 128 x 128, two a CU, 1.0 (448 us in two
+//   rounds), one a CU 0.65; through registers (operands not in vectors) 1.6; the ring of 64 x 64, one a CU, 0.42 (64 x 14336 x
+//   4096: 27.8 us in one round of 64 steps; as 128 x 128 tiles in four parts 34.9).  A round's ramp and end 4 (ring 2.5); joining
+//   the parts 4 and what they take to be written and read at 5 TB/s.
+//   Up to 8 rows (16 where the ring cannot serve them) k_product_rows: 1 x 4096 x 14336 25.3 us against 27.5 as a ring in four
+//   parts; 16 x 14336 x 4096 34.7 against 26.
+Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along, bool direct)
 {
-    uint32_t s = 1;
-    while (tiles * s < 256 && steps / (2 * s) >= 8 && s < 16) s *= 2;
-    return s;
+    const uint32_t steps = std::max(1u, up(uint64_t(depth), uint64_t(kStep / es)));
+    if (along && m <= (direct ? 8 : 16)) return Shape{16, 1, steps};
+    Shape best{128, 1, steps};
+    double least = 1e30;
+    for (const uint32_t tile : {64u, 128u, 256u}) {
+        if ((tile != 128 && !direct) || (tile == 64 && !along)) continue;
+        const uint64_t tiles = uint64_t(up(m, tile)) * up(n, tile);
+        for (uint32_t s = 1; s <= 16 && (s == 1 || (steps / s >= 4 && tiles * s <= 512)); s *= 2) {
+            const uint32_t each = up(steps, s);
+            const double rounds = double((tiles * s + 255) / 256);       // of one workgroup a CU
+            double t = tile == 64 ? rounds * (0.42 * each + 2.5) : (tile == 256 ? rounds * (1.5 * each + 4) : 0);
+            if (tile == 128) t = (direct ? double(uint64_t(rounds) / 2) + 0.65 * double(uint64_t(rounds) % 2) : 0.8 * (rounds + 1)) * each + 2 * (rounds + 1);
+            if (s > 1) t += 4.0 + double(m) * double(n) * s * 8 / 5e6;
+            if (t < least) {
+                least = t;
+                best = Shape{tile, s, each};
+            }
+        }
+    }
+    return best;
 }
 
-Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool direct)
-{
-    Shape s{128, 128, 1, 0, direct};
-    const uint32_t steps = up(uint64_t(depth), uint64_t(kStep / es));
-    const uint64_t tiles = uint64_t(up(m, s.tm)) * up(n, s.tn);
-    s.splits = splits_for(tiles, steps);
-    s.split_steps = up(steps, s.splits);
-    return s;
-}
-
-size_t work_for(int64_t m, int64_t n, int64_t depth, int64_t es)
+size_t work_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along)
 {
     if (m <= 0 || n <= 0 || depth <= 0) return 0;
-    const Shape s = shape_for(m, n, depth, es, true);
-    return s.splits > 1 ? size_t(s.splits) * size_t(m) * size_t(n) * sizeof(float) : 0;
+    const uint32_t s = std::max(shape_for(m, n, depth, es, along, true).splits, shape_for(m, n, depth, es, along, false).splits);
+    return s > 1 ? size_t(s) * size_t(m) * size_t(n) * sizeof(float) : 0;
 }
 
 template <typename F>
@@ -69,7 +82,7 @@ int allow_lds(const void *kernel, uint32_t bytes)
 template <Factor F, int TM, int TN, int WM, int WN, bool PA, bool QA, bool DIRECT>
 int launch_tiles(const ProductArgs &a, hipStream_t st)
 {
-    constexpr uint32_t lds = product_lds(TM, TN, WM, WN);
+    constexpr uint32_t lds = product_lds(TM, TN, WM, WN, PA, QA);
     if (const int rc = allow_lds(reinterpret_cast<const void *>(&k_product<F, TM, TN, WM, WN, PA, QA, DIRECT>), lds); rc != HXT_OK) return rc;
     return launched([&] { k_product<F, TM, TN, WM, WN, PA, QA, DIRECT><<<a.tiles_m * a.tiles_n * a.splits, 64 * WM * WN, lds, st>>>(a); });
 }
@@ -80,17 +93,40 @@ bool vectors(const Operand &o, bool across, int64_t es)
     return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.stride % 16 == 0 && (!across || (int64_t(o.rows) * es) % 16 == 0);
 }
 
+template <Factor F, int WAVES>
+int launch_rows(const ProductArgs &a, hipStream_t st)
+{
+    constexpr uint32_t lds = rows_lds(WAVES);
+    return launched([&] { k_product_rows<F, WAVES><<<up(a.e.n, 16), 64 * WAVES, lds, st>>>(a); });
+}
+
+template <Factor F>
+int launch_ring(const ProductArgs &a, hipStream_t st)
+{
+    constexpr uint32_t lds = kRing * 2 * 64 * kStep;
+    if (const int rc = allow_lds(reinterpret_cast<const void *>(&k_product_ring<F>), lds); rc != HXT_OK) return rc;
+    return launched([&] { k_product_ring<F><<<a.tiles_m * a.tiles_n * a.splits, 256, lds, st>>>(a); });
+}
+
 template <Factor F, bool PA, bool QA>
 int run_product(ProductArgs a, float *work, hipStream_t st)
 {
     constexpr int64_t es = F == F_E4M3 ? 1 : 2;
-    const Shape s = shape_for(a.e.m, a.e.n, a.p.depth, es, vectors(a.p, PA, es) && vectors(a.q, QA, es));
-    a.tiles_m = up(a.e.m, s.tm);
-    a.tiles_n = up(a.e.n, s.tn);
+    const bool direct = vectors(a.p, PA, es) && vectors(a.q, QA, es);
+    const Shape s = shape_for(a.e.m, a.e.n, a.p.depth, es, !PA && !QA, direct);
+    a.tiles_m = up(a.e.m, s.tile);
+    a.tiles_n = up(a.e.n, s.tile);
     a.splits = s.splits;
     a.split_steps = s.split_steps;
     a.work = work;
-    const int rc = s.direct ? launch_tiles<F, 128, 128, 2, 2, PA, QA, true>(a, st) : launch_tiles<F, 128, 128, 2, 2, PA, QA, false>(a, st);
+    int rc;
+    if constexpr (!PA && !QA)          // 16 waves where the workgroups do not fill the chip twice
+        if (s.tile == 16) return a.e.n <= 8192 ? launch_rows<F, 16>(a, st) : launch_rows<F, 8>(a, st);
+    if (!direct) rc = launch_tiles<F, 128, 128, 2, 2, PA, QA, false>(a, st);
+    else if (s.tile == 256) rc = launch_tiles<F, 256, 256, 2, 4, PA, QA, true>(a, st);
+    else if (s.tile == 128) rc = launch_tiles<F, 128, 128, 2, 2, PA, QA, true>(a, st);
+    else if constexpr (!PA && !QA) rc = launch_ring<F>(a, st);
+    else rc = HXT_EUNSUPPORTED;        // (not reached: rings are for operands along)
     if (rc != HXT_OK || a.splits <= 1) return rc;
     const uint64_t groups = uint64_t((a.e.n + 3) / 4) * a.e.m;
     return launched([&] { k_product_join<<<up(groups, 256), 256, 0, st>>>(work, a.splits, a.e); });
@@ -285,8 +321,7 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
     }
     if (x.dbias && x.n > 0) {
         const uint32_t bands = x.m > 0 ? bias_bands(x.m, x.n) : 0;
-        if ((rc = launched([&] { k_product_dbias<<<up(uint64_t(x.n), 256), 256, 0, st>>>(partial, bands, uint32_t(x.n), x.dbias_add, x.dbias); })) != HXT_OK)
-            return rc;
+        if ((rc = operator_column_sums(partial, bands, uint32_t(x.n), x.dbias_add, x.dbias, st)) != HXT_OK) return rc;
     }
     if (x.da && x.m > 0 && x.k > 0) {
         ProductArgs a;
@@ -318,7 +353,7 @@ extern "C" {
 size_t hxt_product_work_bytes(int64_t m, int64_t n, int64_t k, hxt_dtype_t dtype)
 {
     if (check_sizes(m, n, k) != HXT_OK || (dtype != HXT_BF16 && dtype != HXT_E4M3)) return 0;
-    return work_for(m, n, k, element_size(dtype));
+    return work_for(m, n, k, element_size(dtype), true);
 }
 
 int hxt_product(const hxt_product_t *x, void *stream)
@@ -354,7 +389,7 @@ size_t hxt_product_grad_work_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (check_sizes(m, n, k) != HXT_OK || check_sizes(m, k, n) != HXT_OK || check_sizes(n, k, m) != HXT_OK) return 0;
     if (m == 0 || n == 0) return 0;
-    return partial_bytes(m, n) + std::max(work_for(m, k, n, 2), work_for(n, k, m, 2));
+    return partial_bytes(m, n) + std::max(work_for(m, k, n, 2, false), work_for(n, k, m, 2, false));
 }
 
 int hxt_product_grad(const hxt_product_grad_t *x, void *stream)

@@ -35,7 +35,8 @@ def exact(a, b, a_scale=None, b_scale=None, bias=None, act="none", residual=None
 
 
 SIZES = [(1, 1, 1), (1, 16, 8), (3, 5, 7), (1, 256, 1000), (2, 17, 64), (16, 64, 128), (17, 130, 65), (61, 200, 96), (64, 129, 512), (127, 128, 72),
-         (128, 127, 1), (129, 257, 136), (255, 64, 130), (256, 256, 64), (257, 520, 192), (300, 1000, 1023), (1, 4096, 4096), (16, 1024, 2048), (33, 96, 2056)]
+         (128, 127, 1), (129, 257, 136), (255, 64, 130), (256, 256, 64), (257, 520, 192), (300, 1000, 1023), (1, 4096, 4096), (16, 1024, 2048), (33, 96, 2056),
+         (9, 200, 4160), (48, 1000, 1088), (100, 14336, 200), (1100, 1096, 5200), (4100, 4104, 136), (1, 9000, 130)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
@@ -154,7 +155,7 @@ def test_product_into_a_message(m, n, k, lanes, chunk, out):
         assert sums is None or torch.equal(sums, want_sums)
 
 
-GRADS = [(1, 1, 1), (1, 64, 8), (5, 7, 3), (17, 130, 65), (64, 128, 256), (129, 136, 72), (200, 264, 520), (300, 1000, 96), (1021, 100, 51), (2100, 16, 24)]
+GRADS = [(1, 1, 1), (1, 64, 8), (5, 7, 3), (17, 130, 65), (64, 128, 256), (129, 136, 72), (200, 264, 520), (300, 1000, 96), (1021, 100, 51), (2100, 16, 24), (4104, 4160, 264), (264, 4112, 4104)]
 
 
 @pytest.mark.parametrize("m,n,k", GRADS)
