@@ -1620,6 +1620,11 @@ int operator_message(const hxt_plan_t *plan, const void *packed) { return check_
 
 const Plan &operator_plan(const hxt_plan_t *plan) { return plan->p; }
 
+bool operator_packed_nontemporal(const hxt_plan_t *plan, bool load)
+{
+    return load && plan->nt_packed < 0 ? launch_bytes(plan->p) > kOperatorCacheableLoads : ::packed_nontemporal(*plan, load);
+}
+
 int operator_sums(const hxt_plan_t *plan, const void *packed, uint64_t *sums, bool send, hipStream_t st)
 {
     return checksum_pass(*const_cast<hxt_plan_t *>(plan), static_cast<const uint8_t *>(packed), sums, send ? OP_PACK : OP_UNPACK, st);

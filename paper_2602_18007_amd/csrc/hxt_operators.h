@@ -1,4 +1,4 @@
-// What the operators at the ends of a stage (hxt_norm.hip, hxt_product.hip) share: checks of their arguments, places in a
+// What the operators at the ends of a stage (hxt_norm.hip, hxt_norm_grad.hip, hxt_product.hip) share: checks of their arguments, places in a
 // packed buffer, number formats, and the parts of the plan's bookkeeping that hxt_device.hip lends them.
 #ifndef HXT_OPERATORS_H
 #define HXT_OPERATORS_H
@@ -17,12 +17,13 @@ int operator_fail(hipError_t e);                                           // re
 int operator_device();                                                     // HXT_EHIP if there is no HIP device
 int operator_message(const hxt_plan_t *plan, const void *packed);          // the checks of hxt_pack / hxt_unpack
 const Plan &operator_plan(const hxt_plan_t *plan);
+bool operator_packed_nontemporal(const hxt_plan_t *plan, bool load);       // the packed side's cache hint
 // Sums of a packed buffer by a pass of its own, with the accumulators of hxt_pack (send) or hxt_unpack.
 int operator_sums(const hxt_plan_t *plan, const void *packed, uint64_t *sums, bool send, hipStream_t st);
 // Calls enqueue(ctx, cx) while the accumulators of hxt_unpack are this call's.
 int operator_unpack_sums(const hxt_plan_t *plan, uint64_t *sums, hipStream_t st, void (*enqueue)(void *ctx, const SumCtx &cx), void *ctx);
 
-// to[c] = add[c] (nullptr: 0) + the sum over n rows of partial[.][c], in an order fixed by n (hxt_norm.hip).
+// to[c] = add[c] (nullptr: 0) + the sum over n rows of partial[.][c], in an order fixed by n (hxt_norm_grad.hip).
 int operator_column_sums(const float *partial, uint32_t n, uint32_t cols, const float *add, float *to, hipStream_t st);
 
 // ---- argument checks (host) ----------------------------------------------------------
@@ -157,10 +158,14 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x)
 {
     return wave_total(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t v)
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v)       // the total in lane 63
 {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_down(v, o, 64);
-    return v;                                          // in lane 0
+    v = dpp_plus<0x111>(v);
+    v = dpp_plus<0x112>(v);
+    v = dpp_plus<0x114>(v);
+    v = dpp_plus<0x118>(v);
+    v = dpp_plus<0x142>(v);
+    return dpp_plus<0x143>(v);
 }
 
 }  // namespace hxt

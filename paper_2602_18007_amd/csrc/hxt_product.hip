@@ -20,6 +20,7 @@ int64_t element_size(hxt_dtype_t t) { return t == HXT_BF16 ? 2 : (t == HXT_F32 ?
 struct Shape {
     uint32_t tile;                 // 16: k_product_rows, 64: k_product_ring, else k_product's
     uint32_t splits, split_steps;
+    double us;                     // what it is expected to take
 };
 
 uint32_t up(uint64_t n, uint64_t to) { return uint32_t((n + to - 1) / to); }
@@ -35,8 +36,8 @@ uint32_t up(uint64_t n, uint64_t to) { return uint32_t((n + to - 1) / to); }
 Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along, bool direct)
 {
     const uint32_t steps = std::max(1u, up(uint64_t(depth), uint64_t(kStep / es)));
-    if (along && m <= (direct ? 8 : 16)) return Shape{16, 1, steps};
-    Shape best{128, 1, steps};
+    if (along && m <= (direct ? 8 : 16)) return Shape{16, 1, steps, 0};
+    Shape best{128, 1, steps, 0};
     double least = 1e30;
     for (const uint32_t tile : {64u, 128u, 256u}) {
         if ((tile != 128 && !direct) || (tile == 64 && !along)) continue;
@@ -49,18 +50,44 @@ Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along, boo
             if (s > 1) t += 4.0 + double(m) * double(n) * s * 8 / 5e6;
             if (t < least) {
                 least = t;
-                best = Shape{tile, s, each};
+                best = Shape{tile, s, each, t};
             }
         }
     }
     return best;
 }
 
-size_t work_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along)
+uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
+
+uint64_t parts_bytes(const Shape &s, int64_t m, int64_t n) { return s.splits > 1 ? up256(uint64_t(s.splits) * m * n * sizeof(float)) : 0; }
+
+// A copy of rows x cols elements whose rows begin at 16-byte multiples.
+uint64_t copy_bytes(int64_t rows, int64_t cols, int64_t es) { return up256(uint64_t(rows) * ((uint64_t(cols * es) + 15) / 16 * 16)); }
+
+// Operands whose rows are not in vectors (odd row lengths or pitches) are copied first where the workspace has room and the
+// copies, written and read at 4.5 TB/s, cost less than the way through registers (4096 x 4096 x 4095: 246 us through registers,
+// 131 copied).  s: the way without copies, and after the call the chosen one.
+bool worth_copying(Shape &s, int64_t m, int64_t n, int64_t depth, int64_t es, bool along, uint64_t copied)
+{
+    Shape with = shape_for(m, n, depth, es, along, true);
+    with.us += 3 + double(copied) * 2 / 4.5e6;
+    if (s.tile == 16 || with.us >= s.us) return false;
+    s = with;
+    return true;
+}
+
+// Workspace of a product: the parts of its sums; and of operands that cannot be in vectors as they are (p_cols, q_cols: elements
+// that lie next to each other in them) the copies.
+size_t work_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool p_across, bool q_across)
 {
     if (m <= 0 || n <= 0 || depth <= 0) return 0;
-    const uint32_t s = std::max(shape_for(m, n, depth, es, along, true).splits, shape_for(m, n, depth, es, along, false).splits);
-    return s > 1 ? size_t(s) * size_t(m) * size_t(n) * sizeof(float) : 0;
+    const bool along = !p_across && !q_across;
+    Shape direct = shape_for(m, n, depth, es, along, true), any = shape_for(m, n, depth, es, along, false);
+    uint64_t need = std::max(parts_bytes(direct, m, n), parts_bytes(any, m, n)), copies = 0;
+    for (const auto &[across, outer] : {std::pair{p_across, m}, {q_across, n}})
+        if ((across ? outer : depth) * es % 16) copies += across ? copy_bytes(depth, outer, es) : copy_bytes(outer, depth, es);
+    if (copies && worth_copying(any, m, n, depth, es, along, copies)) need = std::max(need, parts_bytes(any, m, n) + copies);
+    return size_t(need);
 }
 
 template <typename F>
@@ -108,17 +135,46 @@ int launch_ring(const ProductArgs &a, hipStream_t st)
     return launched([&] { k_product_ring<F><<<a.tiles_m * a.tiles_n * a.splits, 256, lds, st>>>(a); });
 }
 
+// Copies an operand's rows to `to`.
+template <Factor F>
+int align_rows(Operand &o, bool across, uint8_t *to, hipStream_t st)
+{
+    using E = std::conditional_t<F == F_E4M3, uint8_t, uint16_t>;
+    const uint32_t rows = across ? o.depth : o.rows, cols = across ? o.rows : o.depth, vectors = up(uint64_t(cols) * sizeof(E), 16);
+    const uint64_t count = uint64_t(rows) * vectors;
+    const int rc = launched([&] { k_product_align<E><<<up(count, 256), 256, 0, st>>>(o.p, o.stride, cols, count, vectors, reinterpret_cast<u32x4 *>(to)); });
+    o.p = to;
+    o.stride = int64_t(vectors) * 16;
+    if (across) o.rows = uint32_t(vectors * 16 / sizeof(E));           // (the zeros behind are columns of their own, not stored)
+    return rc;
+}
+
 template <Factor F, bool PA, bool QA>
-int run_product(ProductArgs a, float *work, hipStream_t st)
+int run_product(ProductArgs a, uint8_t *work, size_t work_bytes, hipStream_t st)
 {
     constexpr int64_t es = F == F_E4M3 ? 1 : 2;
-    const bool direct = vectors(a.p, PA, es) && vectors(a.q, QA, es);
-    const Shape s = shape_for(a.e.m, a.e.n, a.p.depth, es, !PA && !QA, direct);
+    const int64_t m = a.e.m, n = a.e.n, depth = a.p.depth;
+    const bool p_direct = vectors(a.p, PA, es), q_direct = vectors(a.q, QA, es);
+    bool direct = p_direct && q_direct;
+    Shape s = shape_for(m, n, depth, es, !PA && !QA, direct);
+    if (!direct) {
+        const uint64_t p_bytes = p_direct ? 0 : (PA ? copy_bytes(depth, m, es) : copy_bytes(m, depth, es));
+        const uint64_t q_bytes = q_direct ? 0 : (QA ? copy_bytes(depth, n, es) : copy_bytes(n, depth, es));
+        Shape copied = s;
+        if (worth_copying(copied, m, n, depth, es, !PA && !QA, p_bytes + q_bytes) && parts_bytes(copied, m, n) + p_bytes + q_bytes <= work_bytes) {
+            s = copied;
+            direct = true;
+            uint8_t *at = work + parts_bytes(s, m, n);
+            int rc;
+            if (!p_direct && (rc = align_rows<F>(a.p, PA, at, st)) != HXT_OK) return rc;
+            if (!q_direct && (rc = align_rows<F>(a.q, QA, at + p_bytes, st)) != HXT_OK) return rc;
+        }
+    }
     a.tiles_m = up(a.e.m, s.tile);
     a.tiles_n = up(a.e.n, s.tile);
     a.splits = s.splits;
     a.split_steps = s.split_steps;
-    a.work = work;
+    a.work = reinterpret_cast<float *>(work);
     int rc;
     if constexpr (!PA && !QA)          // 16 waves where the workgroups do not fill the chip twice
         if (s.tile == 16) return a.e.n <= 8192 ? launch_rows<F, 16>(a, st) : launch_rows<F, 8>(a, st);
@@ -129,7 +185,7 @@ int run_product(ProductArgs a, float *work, hipStream_t st)
     else rc = HXT_EUNSUPPORTED;        // (not reached: rings are for operands along)
     if (rc != HXT_OK || a.splits <= 1) return rc;
     const uint64_t groups = uint64_t((a.e.n + 3) / 4) * a.e.m;
-    return launched([&] { k_product_join<<<up(groups, 256), 256, 0, st>>>(work, a.splits, a.e); });
+    return launched([&] { k_product_join<<<up(groups, 256), 256, 0, st>>>(a.work, a.splits, a.e); });
 }
 
 Operand operand(const Matrix &m, bool across)
@@ -152,7 +208,7 @@ struct Product {
           a_scale(x.a_scale, 1, x.m, 0, 4), b_scale(x.b_scale, 1, x.n, 0, 4), bias(x.bias, 1, x.n, 0, 2),
           residual(x.residual, x.m, x.n, x.residual_stride, element_size(x.out_dtype)), pre(x.pre, x.m, x.n, x.pre_stride, 2),
           c(x.c, x.m, x.n, x.c_stride, element_size(x.out_dtype)),
-          work(x.work, 1, int64_t(hxt_product_work_bytes(x.m, x.n, x.k, x.dtype)), 0, 1)
+          work(x.work, 1, x.work ? int64_t(x.work_bytes) : 0, 0, 1)
     {
     }
 };
@@ -187,8 +243,8 @@ int check_product(const hxt_product_t *x, bool message)
     }
     for (const Matrix *r : {&p.a_scale, &p.b_scale, &p.bias})
         if ((rc = check_read(*r)) != HXT_OK) return rc;
-    if (p.work.cols && (!x->work || x->work_bytes < size_t(p.work.cols))) return HXT_EINVAL;
-    if (p.work.cols && p.work.p % 16) return HXT_EALIGN;
+    if (x->work_bytes > (size_t(1) << 62) || p.work.cols < int64_t(hxt_product_work_bytes(x->m, x->n, x->k, x->dtype))) return HXT_EINVAL;
+    if (p.work.p % 16) return HXT_EALIGN;
     for (const Matrix *out : {&p.pre, &p.c, &p.work}) {
         for (const Matrix *in : {&p.a, &p.b, &p.a_scale, &p.b_scale, &p.bias})
             if (!out->disjoint(*in)) return HXT_EOVERLAP;
@@ -221,8 +277,8 @@ int launch_forward(const hxt_product_t &x, const Plan *plan, void *packed, hipSt
     e.out32 = x.out_dtype == HXT_F32;
     e.message = plan != nullptr;
     if (plan) e.g = plan->geom;
-    float *work = static_cast<float *>(x.work);
-    return x.dtype == HXT_E4M3 ? run_product<F_E4M3, false, false>(a, work, st) : run_product<F_BF16, false, false>(a, work, st);
+    uint8_t *work = static_cast<uint8_t *>(x.work);
+    return x.dtype == HXT_E4M3 ? run_product<F_E4M3, false, false>(a, work, p.work.cols, st) : run_product<F_BF16, false, false>(a, work, p.work.cols, st);
 }
 
 // ---- gradients ---------------------------------------------------------------------------------
@@ -242,7 +298,7 @@ struct ProductGrad {
           a(x.db ? x.a : nullptr, x.m, x.k, x.a_stride, 2), b(x.da ? x.b : nullptr, x.n, x.k, x.b_stride, 2), dz(x.dz, x.m, x.n, x.dz_stride, 2),
           da(x.da, x.m, x.k, x.da_stride, 2), db(x.db, x.n, x.k, x.db_stride, element_size(x.db_dtype)),
           db_add(x.db ? x.db_add : nullptr, x.n, x.k, x.db_add_stride, element_size(x.db_dtype)), dbias(x.dbias, 1, x.n, 0, 4),
-          dbias_add(x.dbias ? x.dbias_add : nullptr, 1, x.n, 0, 4), work(x.work, 1, int64_t(hxt_product_grad_work_bytes(x.m, x.n, x.k)), 0, 1)
+          dbias_add(x.dbias ? x.dbias_add : nullptr, 1, x.n, 0, 4), work(x.work, 1, x.work ? int64_t(x.work_bytes) : 0, 0, 1)
     {
     }
 };
@@ -268,8 +324,8 @@ int check_product_grad(const hxt_product_grad_t *x)
     }
     for (const Matrix *r : {&p.dbias, &p.dbias_add})
         if ((rc = check_read(*r)) != HXT_OK) return rc;
-    if (p.work.cols && (!x->work || x->work_bytes < size_t(p.work.cols))) return HXT_EINVAL;
-    if (p.work.cols && p.work.p % 16) return HXT_EALIGN;
+    if (x->work_bytes > (size_t(1) << 62) || p.work.cols < int64_t(hxt_product_grad_work_bytes(x->m, x->n, x->k))) return HXT_EINVAL;
+    if (p.work.p % 16) return HXT_EALIGN;
     const Matrix *outs[] = {&p.dz, &p.da, &p.db, &p.dbias, &p.work};
     for (const Matrix *out : outs) {
         for (const Matrix *in : {&p.dc, &p.pre, &p.a, &p.b, &p.db_add, &p.dbias_add}) {
@@ -299,7 +355,8 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
     const ProductGrad p(x);
     int rc;
     float *partial = static_cast<float *>(x.work);
-    float *work = x.work ? reinterpret_cast<float *>(static_cast<uint8_t *>(x.work) + partial_bytes(x.m, x.n)) : nullptr;
+    uint8_t *work = x.work ? static_cast<uint8_t *>(x.work) + partial_bytes(x.m, x.n) : nullptr;
+    const size_t room = x.work ? x.work_bytes - std::min(x.work_bytes, partial_bytes(x.m, x.n)) : 0;
     Matrix dz = p.dz;                                    // what the products read
     if (x.act == HXT_ACT_NONE) dz = p.dc;
     const bool copies = x.act != HXT_ACT_NONE;
@@ -330,7 +387,7 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
         a.q = operand_read(p.b, true);
         a.p.depth = a.q.depth = uint32_t(x.n);
         a.e = plain(p.da, false);
-        if ((rc = run_product<F_BF16, false, true>(a, work, st)) != HXT_OK) return rc;
+        if ((rc = run_product<F_BF16, false, true>(a, work, room, st)) != HXT_OK) return rc;
     }
     if (x.db && x.n > 0 && x.k > 0) {
         ProductArgs a;
@@ -341,7 +398,7 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
         a.e = plain(p.db, x.db_dtype == HXT_F32);
         a.e.residual = reinterpret_cast<const uint8_t *>(p.db_add.p);
         a.e.residual_stride = x.db_add_stride * p.db_add.es;
-        if ((rc = run_product<F_BF16, true, true>(a, work, st)) != HXT_OK) return rc;
+        if ((rc = run_product<F_BF16, true, true>(a, work, room, st)) != HXT_OK) return rc;
     }
     return HXT_OK;
 }
@@ -353,7 +410,7 @@ extern "C" {
 size_t hxt_product_work_bytes(int64_t m, int64_t n, int64_t k, hxt_dtype_t dtype)
 {
     if (check_sizes(m, n, k) != HXT_OK || (dtype != HXT_BF16 && dtype != HXT_E4M3)) return 0;
-    return work_for(m, n, k, element_size(dtype), true);
+    return work_for(m, n, k, element_size(dtype), false, false);
 }
 
 int hxt_product(const hxt_product_t *x, void *stream)
@@ -389,7 +446,7 @@ size_t hxt_product_grad_work_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (check_sizes(m, n, k) != HXT_OK || check_sizes(m, k, n) != HXT_OK || check_sizes(n, k, m) != HXT_OK) return 0;
     if (m == 0 || n == 0) return 0;
-    return partial_bytes(m, n) + std::max(work_for(m, k, n, 2, false), work_for(n, k, m, 2, false));
+    return partial_bytes(m, n) + std::max(work_for(m, k, n, 2, false, true), work_for(n, k, m, 2, true, true));
 }
 
 int hxt_product_grad(const hxt_product_grad_t *x, void *stream)

@@ -760,6 +760,27 @@ __global__ __launch_bounds__(256) void k_product_join(const float *__restrict__ 
     finish<4>(e, m, n0, z);
 }
 
+// Rows copied to 16-byte multiples, vectors a row, zeros behind the row's end.
+template <typename E>
+__global__ __launch_bounds__(256) void k_product_align(const uint8_t *__restrict__ from, int64_t stride, uint32_t cols, uint64_t count, uint32_t vectors,
+                                                       u32x4 *__restrict__ to)
+{
+    const uint64_t id = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (id >= count) return;
+    constexpr uint32_t V = 16 / sizeof(E);
+    const uint64_t row = id / vectors;
+    const uint32_t col = uint32_t(id - row * vectors) * V;
+    const uint8_t *at = from + row * stride + size_t(col) * sizeof(E);
+    if (col + V <= cols) {
+        to[id] = load16_any<false>(at);
+        return;
+    }
+    E e[V];
+#pragma unroll
+    for (uint32_t i = 0; i < V; ++i) e[i] = col + i < cols ? reinterpret_cast<const E *>(at)[i] : E(0);
+    to[id] = __builtin_bit_cast(u32x4, e);
+}
+
 // ---- dz and the bias gradient ----------------------------------------------------------------
 struct DzArgs {
     uint32_t m, n;

@@ -34,6 +34,11 @@ constexpr uint64_t kCacheableMisalignedLoads = uint64_t(64) << 20;
 constexpr uint64_t kCacheablePackedLoads = uint64_t(128) << 20, kCacheablePackedPasses = uint64_t(64) << 20;
 constexpr uint64_t kWrittenThroughLimit = uint64_t(1) << 30;
 
+// Norms of received messages read the packed side cacheable only up to 16 MiB: what they write beside it pushes it out (pack + norm
+// of 2 tensors, with a sum and 8 bits as outputs, cacheable against non-temporal: 16 MiB 18.0 and 18.1 us, 64 MiB 45.9 and 42.2, 112
+// MiB 75.5 and 67.8).
+constexpr uint64_t kOperatorCacheableLoads = uint64_t(16) << 20;
+
 // Bytes a launch over the message moves on the packed side (its packed buffer, whole chunks, can be much longer).
 inline uint64_t launch_bytes(const Plan &p) { return p.L; }
 

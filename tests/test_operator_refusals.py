@@ -115,6 +115,9 @@ def test_product_wants_its_workspace():
         assert status("hxt_product", product_block(work=at(7), work_bytes=need - 1, **kw)) == hxt.HXT_EINVAL
         assert status("hxt_product", product_block(work=at(7) + 4, work_bytes=need, **kw)) == hxt.HXT_EALIGN
         assert status("hxt_product", product_block(work=at(1), work_bytes=need, **kw)) == hxt.HXT_EOVERLAP
+    # more than is needed may be used: none of it may be another argument's
+    assert status("hxt_product", product_block(work=at(1) - 4096, work_bytes=8192)) == hxt.HXT_EOVERLAP
+    assert status("hxt_product", product_block(work=at(7) + 8, work_bytes=8192)) == hxt.HXT_EALIGN
 
 
 @NO_GPU
