@@ -20,6 +20,7 @@ int64_t element_size(hxt_dtype_t t) { return t == HXT_BF16 ? 2 : (t == HXT_F32 ?
 struct Shape {
     uint32_t tile;                 // 16: k_product_rows, 64: k_product_ring, else k_product's
     uint32_t splits, split_steps;
+    uint32_t half;                 // of 256 x 256 tiles: columns of tiles at the end that go as 256 x 128
     double us;                     // what it is expected to take
 };
 
@@ -27,17 +28,19 @@ uint32_t up(uint64_t n, uint64_t to) { return uint32_t((n + to - 1) / to); }
 
 // Which kernel, and in how many parts of the contraction: the least time by these measured costs in us.
 //   A step (128 bytes of the contraction) of a full round of workgroups, a round being what the chip holds at a time:
-//   256 x 256 tiles, one a CU, 1.5 (4096 x 4096 x 14336: 341 us in one round of 224 steps); 128 x 128, two a CU, 1.0 (448 us in two
+//   256 x 256 tiles, one a CU, 1.5 (4096 x 4096 x 14336: 341 us in one round of 224 steps), 256 x 128 0.9; 128 x 128, two a CU, 1.0 (448 us in two
 //   rounds), one a CU 0.65; through registers (operands not in vectors) 1.6; the ring of 64 x 64, one a CU, 0.42 (64 x 14336 x
 //   4096: 27.8 us in one round of 64 steps; as 128 x 128 tiles in four parts 34.9).  A round's ramp and end 4 (ring 2.5); joining
-//   the parts 4 and what they take to be written and read at 5 TB/s.
-//   Up to 8 rows (16 where the ring cannot serve them) k_product_rows: 1 x 4096 x 14336 25.3 us against 27.5 as a ring in four
-//   parts; 16 x 14336 x 4096 34.7 against 26.
+//   the parts 4 and what they take to be written and read at 5 TB/s.  Where whole rounds of 256 x 256 tiles leave few, these go as
+//   256 x 128 in a launch of their own (8 bits, 4096 x 14336 x 4096: 213 -> 202 us; bf16 387 -> 385, where the clock gives back what
+//   a half-empty round leaves).
+//   Up to 4 rows (16 where the ring cannot serve them) k_product_rows: 1 x 4096 x 14336 23.6 us against 27.5 as a ring in four
+//   parts; 8 x 14336 x 4096 29.5 against 26.
 Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along, bool direct)
 {
     const uint32_t steps = std::max(1u, up(uint64_t(depth), uint64_t(kStep / es)));
-    if (along && m <= (direct ? 8 : 16)) return Shape{16, 1, steps, 0};
-    Shape best{128, 1, steps, 0};
+    if (along && m <= (direct ? 4 : 16)) return Shape{16, 1, steps, 0, 0};
+    Shape best{128, 1, steps, 0, 0};
     double least = 1e30;
     for (const uint32_t tile : {64u, 128u, 256u}) {
         if ((tile != 128 && !direct) || (tile == 64 && !along)) continue;
@@ -50,7 +53,16 @@ Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along, boo
             if (s > 1) t += 4.0 + double(m) * double(n) * s * 8 / 5e6;
             if (t < least) {
                 least = t;
-                best = Shape{tile, s, each, t};
+                best = Shape{tile, s, each, 0, t};
+            }
+            // what is left behind whole rounds, in half tiles that fill one
+            const uint64_t tm = up(m, 256), tn = up(n, 256), whole = tile == 256 && s == 1 ? tiles / 256 * 256 / tm : 0;
+            if (whole && whole < tn && (tn - whole) * 2 * tm <= 256) {
+                const double u = double((tm * whole + 255) / 256) * (1.5 * each + 4) + 0.9 * each + 8;
+                if (u < least) {
+                    least = u;
+                    best = Shape{tile, s, each, uint32_t(tn - whole), u};
+                }
             }
         }
     }
@@ -179,7 +191,15 @@ int run_product(ProductArgs a, uint8_t *work, size_t work_bytes, hipStream_t st)
     if constexpr (!PA && !QA)          // 16 waves where the workgroups do not fill the chip twice
         if (s.tile == 16) return a.e.n <= 8192 ? launch_rows<F, 16>(a, st) : launch_rows<F, 8>(a, st);
     if (!direct) rc = launch_tiles<F, 128, 128, 2, 2, PA, QA, false>(a, st);
-    else if (s.tile == 256) rc = launch_tiles<F, 256, 256, 2, 4, PA, QA, true>(a, st);
+    else if (s.tile == 256) {
+        a.tiles_n -= s.half;
+        rc = launch_tiles<F, 256, 256, 2, 4, PA, QA, true>(a, st);
+        if (rc == HXT_OK && s.half) {
+            a.n_first = a.tiles_n * 256;
+            a.tiles_n = up(n - a.n_first, 128);
+            rc = launch_tiles<F, 256, 128, 4, 2, PA, QA, true>(a, st);
+        }
+    }
     else if (s.tile == 128) rc = launch_tiles<F, 128, 128, 2, 2, PA, QA, true>(a, st);
     else if constexpr (!PA && !QA) rc = launch_ring<F>(a, st);
     else rc = HXT_EUNSUPPORTED;        // (not reached: rings are for operands along)

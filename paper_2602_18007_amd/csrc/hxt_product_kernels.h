@@ -41,6 +41,7 @@ struct Epilogue {
 struct ProductArgs {
     Operand p, q;
     uint32_t tiles_m, tiles_n;
+    uint32_t n_first;             // column of the first tile
     uint32_t splits;              // parts of the contraction; > 1: partial sums go to work[split][m][n]
     uint32_t split_steps;         // steps of one part
     float *work;
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs a)
     const uint32_t split = a.splits > 1 ? blockIdx.x / tiles : 0;
     uint32_t ti, tj;
     tile_at(blockIdx.x - split * tiles, tiles, a.tiles_m, a.tiles_n, ti, tj);
-    const uint32_t m0 = ti * TM, n0 = tj * TN;
+    const uint32_t m0 = ti * TM, n0 = a.n_first + tj * TN;
     const int wave = int(threadIdx.x) >> 6, wm = wave / WN, wn = wave % WN;
     const uint32_t depth = a.p.depth, all_steps = (depth + TileP::DEPTH - 1) / TileP::DEPTH;
     const uint32_t first = split * a.split_steps, last = min(all_steps, first + a.split_steps);
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs a)
         finish_rows<ROUND, COLS, PITCH>(a, split, mine, m0 + wm * ROWS + r0, n0 + wn * COLS);
         __builtin_amdgcn_wave_barrier();
     }
-    if (a.splits <= 1 && a.e.message && blockIdx.x == 0) pad_message(a.e);
+    if (a.splits <= 1 && a.e.message && blockIdx.x == 0 && !a.n_first) pad_message(a.e);
 }
 
 // ---- tens of rows -------------------------------------------------------------------------------
@@ -662,7 +663,8 @@ __global__ __launch_bounds__(256) void k_product_ring(ProductArgs a)
 // Products of at most 16 rows: every row of b is read once, straight into the registers of the matrix instruction, and nothing is
 // shared but the rows of a, which stay in the L2.  A workgroup owns 16 columns; its waves take the contraction's 128-byte pieces
 // in turn, and their sums are joined in LDS in the waves' order.  Bound by the reading of b (1 x 4096 x 14336, bf16, 16 waves:
-// 25.3 us, 4.6 TB/s).  Any alignment: the vectors of a fragment are read wherever they lie.
+// 23.6 us, 5.0 TB/s, of which 5 are the ramp and the end; with b read non-temporally 25.4, with 3 pieces a batch 27.3, by 8 waves
+// 26.0).  Any alignment: the vectors of a fragment are read wherever they lie.
 HXT_HD constexpr int rows_lds(int waves) { return waves * 16 * 20 * 4; }
 
 template <Factor F, int WAVES>
@@ -686,7 +688,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product_rows(ProductArgs a)
             const uint64_t at = uint64_t(min(wave + WAVES * (b * UNROLL + u), pieces - 1)) * kStep;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                ys[u][h] = load16_any<true>(at_b + at + 64 * h);
+                ys[u][h] = load16_any<false>(at_b + at + 64 * h);
                 xs[u][h] = load16_any<false>(at_a + at + 64 * h);
             }
         }
