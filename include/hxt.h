@@ -45,7 +45,8 @@
  *     makes the later stream wait for the earlier one (an event), so they never
  *     overlap; the claim of the accumulators and the enqueue of the kernels that
  *     use them are one critical section, so this also holds between threads.
- *     The sets are: hxt_pack; hxt_unpack and hxt_unpack_accumulate; hxt_checksum;
+ *     The sets are: hxt_pack, hxt_pack_norm_grad and hxt_pack_product; hxt_unpack,
+ *     hxt_unpack_accumulate and hxt_unpack_norm; hxt_checksum;
  *     hxt_checksum2, hxt_seal and hxt_pack_seal; hxt_verify and hxt_unpack_verify.
  *     One plan can therefore serve a sending stream and a receiving stream at the
  *     same time; messages that should overlap within one set need a plan each.
@@ -54,7 +55,7 @@
  *     given to such a call must stay alive until the plan is destroyed or until a later
  *     call of the same set has been made on another stream.
  *   - Stream capture: hxt_pack, hxt_unpack, hxt_unpack_accumulate, the batched calls,
- *     the checksum / seal / verify passes and the fused tag calls may be captured into a
+ *     the operators at the ends of a stage (hxt_norm ... hxt_product_grad), the checksum / seal / verify passes and the fused tag calls may be captured into a
  *     HIP graph (they record kernels only, no memset and no copy).  A call that asks for
  *     checksums and finds its accumulator set last used on another stream inserts the
  *     ordering event described above; make the first such call on the capture stream

@@ -248,6 +248,9 @@ int hxt_unpack_norm(const hxt_plan_t *plan, const void *packed, const hxt_norm_t
     if (sum.p % 8) return HXT_EALIGN;
     for (const Matrix *out : {&m.h, &m.y, &m.q, &scale})
         if (!out->disjoint(message) || !out->disjoint(sum)) return HXT_EOVERLAP;
+    const Matrix weight(a->weight, 1, a->cols, 0, m.x.es);
+    for (const Matrix *in : {&m.residual, &weight, &message})
+        if (!in->disjoint(sum)) return HXT_EOVERLAP;
     NormArgs na = norm_args(*a);
     na.g = p.geom;
     na.packed = static_cast<const uint8_t *>(packed);
@@ -256,7 +259,7 @@ int hxt_unpack_norm(const hxt_plan_t *plan, const void *packed, const hxt_norm_t
     na.residual_off = n == 2 ? p.tensors[1].stream_off : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint64_t rb = m.x.row_bytes();
-    if (sums && rb % 16 == 0 && p.B >= rb * uint64_t(rows_of(norm_shape(a->rows, a->cols, m.x.es)))) {       // the sums come with the rows
+    if (sums && rb % 16 == 0 && p.B <= uint64_t(1) << 35 && p.B >= rb * uint64_t(rows_of(norm_shape(a->rows, a->cols, m.x.es)))) {       // the sums come with the rows (and a chunk's vectors are counted in 32 bits)
         struct Enqueue {
             NormArgs &n;
             hxt_dtype_t dtype;

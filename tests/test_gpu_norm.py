@@ -31,8 +31,11 @@ SHAPES = [(1, 1), (3, 5), (1, 64), (7, 65), (5, 511), (4, 512), (6, 520), (3, 10
           (2, 8192), (2, 8200), (2, 16384), (1, 16391), (2, 32768)]
 
 
+MANY_ROWS = [(1030, 600), (1025, 1500), (1027, 4000), (1024, 4096), (1025, 6001), (1026, 12000), (1024, 20008)]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("rows,cols", SHAPES + MANY_ROWS)
 def test_norm_of_tensors(rows, cols, dtype):
     print("norm", rows, cols, dtype, flush=True)
     g = generator(rows * 70001 + cols)
@@ -78,12 +81,12 @@ def test_norm_outputs_alone_in_place_and_broadcast(dtype):
     assert torch.equal(both[:, :cols], x)
 
 
-@pytest.mark.parametrize("cols", [64, 1000, 4096])
-def test_norm_of_rows_with_unusual_values(cols):
+@pytest.mark.parametrize("rows,cols", [(9, 64), (9, 1000), (9, 4096), (1031, 520), (1025, 1100), (1027, 3000), (1025, 5000)])
+def test_norm_of_rows_with_unusual_values(rows, cols):
     """Rows of zeros, of the type's largest and smallest values, with NaN and with infinities; each row apart from the others."""
     for dtype in (BF16, F32):
         big, tiny = torch.finfo(dtype).max, torch.finfo(dtype).tiny
-        x = normal((9, cols), generator(5), 1.0, dtype)
+        x = normal((rows, cols), generator(5), 1.0, dtype)
         x[0] = 0
         x[1] = big / 4
         x[2] = tiny
@@ -93,7 +96,7 @@ def test_norm_of_rows_with_unusual_values(cols):
         x[6] *= 1e25
         x[7, : cols // 2] = 0
         y, h = torch.empty_like(x), torch.empty_like(x)
-        q, scale = torch.empty(9, cols, dtype=E4M3, device=DEV), torch.empty(9, device=DEV)
+        q, scale = torch.empty(rows, cols, dtype=E4M3, device=DEV), torch.empty(rows, device=DEV)
         hxt.hxt_norm(hxt.Norm(None, EPS, x=x, h=h, y=y, q=q, scale=scale))
         H, Y, S = norm_exact(x, None, None, EPS)
         S = torch.where(torch.isnan(Y).any(1), torch.full_like(S, float("nan")), S)
@@ -112,7 +115,8 @@ def packed_of(plan, tensors):
 
 
 MESSAGES = [(1, 4096, 2, 16384), (37, 512, 3, 4096), (64, 1000, 4, 65536), (33, 1001, 2, 768), (5, 4096, 2, 256), (129, 4096, 4, 1 << 20), (4, 8, 2, 256),
-            (19, 3584, 8, 32768), (3, 16384, 2, 1 << 16)]
+            (19, 3584, 8, 32768), (3, 16384, 2, 1 << 16),
+            (1030, 3584, 4, 1 << 18), (1025, 2048, 2, 4096), (1027, 264, 3, 768), (1026, 5000, 2, 1 << 20)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
