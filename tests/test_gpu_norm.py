@@ -335,6 +335,38 @@ def test_norm_repeats_bit_for_bit():
     assert all(torch.equal(a, got[0][0]) and torch.equal(b, got[0][1]) for a, b in got)
 
 
+def test_rows_past_four_gigabytes():
+    """Offsets beyond 32 bits, of tensors and in a message: the rows repeat every 1000, so that all of them are known."""
+    rows, cols, every = 140000, 16384, 1000
+    g = generator(13)
+    base, w = normal((every, cols), g, 1.0, BF16), (1 + 0.2 * normal((cols,), g)).to(BF16)
+    x = base.repeat(rows // every, 1)
+    y = torch.empty_like(x)
+    want = norm_exact(base, None, w, EPS)
+    hxt.hxt_norm(hxt.Norm(w, EPS, x=x, y=y))
+    check_norm(None, y[:every], None, None, want, BF16)
+    assert bool((y.view(-1, every, cols) == y[:every]).all())
+    plan = hxt.hxt_plan((rows, cols), None, BF16, 8, 25 << 20)
+    packed = torch.empty(plan.packed_bytes, dtype=torch.uint8, device=DEV)
+    hxt.hxt_pack(plan, [x], packed)
+    first = y[:every].clone()
+    y.zero_()
+    got, sums = torch.empty(plan.num_chunks, dtype=torch.int64, device=DEV), torch.empty(plan.num_chunks, dtype=torch.int64, device=DEV)
+    hxt.hxt_checksum(plan, packed, got)
+    hxt.hxt_unpack_norm(plan, packed, hxt.Norm(w, EPS, y=y), sums)
+    within(y[:every], want[1], want[1].abs() * (HALF[BF16] + EPS32) + SMALLEST[BF16], "y")
+    assert bool((y.view(-1, every, cols) == y[:every]).all()) and torch.equal(sums, got)
+    del packed, first
+    dx, dweight = torch.empty_like(x), torch.empty(cols, device=DEV)
+    work = torch.empty(hxt.hxt_norm_grad_work_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    hxt.hxt_norm_grad(hxt.NormGrad(w, EPS, h=x, dy=x, dx=dx, dweight=dweight, work=work))
+    check_grad(dx[:every], None, base, base, None, w, BF16)
+    assert bool((dx.view(-1, every, cols) == dx[:every]).all())
+    _, _, DW, size = norm_grad_exact(base, base, None, w, EPS)
+    # 140000 rows over 512 workgroups: 274 additions each, then 64 and 8
+    within(dweight, DW * (rows // every), size * (rows // every) * (400 * 2.0 ** -24 + 2 * EPS32), "dweight")
+
+
 def test_the_binding_refuses_tensors_of_the_host():
     x = torch.zeros(4, 64)
     with pytest.raises(ValueError):

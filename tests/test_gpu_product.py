@@ -280,6 +280,27 @@ def test_product_grad_of_nothing():
     assert bool((da == 0).all())
 
 
+def test_results_past_four_gigabytes():
+    """Offsets beyond 32 bits in results, gradients and factors: the rows repeat every 512, so that all of them are known."""
+    m, n, k, every = 71680, 32768, 64, 512
+    g = generator(21)
+    base, b = whole((every, k), g).to(BF16), whole((n, k), g).to(BF16)
+    a = base.repeat(m // every, 1)
+    c = torch.empty(m, n, dtype=BF16, device=DEV)
+    hxt.hxt_product(hxt.Product(a, b, c=c, work=workspace(m, n, k).m.view(-1)))
+    assert torch.equal(c[:every], exact(base, b)[0].to(F32).to(BF16))
+    assert bool((c.view(-1, every, n) == c[:every]).all())
+    rows = whole((every, n), g, 1).to(BF16)
+    c.copy_(rows.repeat(m // every, 1))
+    da, dbias = torch.empty(m, k, dtype=BF16, device=DEV), torch.empty(n, device=DEV)
+    db = torch.empty(n, k, device=DEV)
+    work = torch.empty(hxt.hxt_product_grad_work_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(c, a, b, da=da, db=db, dbias=dbias, work=work))
+    assert torch.equal(da[:every], (f64(rows) @ f64(b)).to(F32).to(BF16)) and bool((da.view(-1, every, k) == da[:every]).all())
+    assert torch.equal(db, (f64(rows).t().contiguous() @ f64(base) * (m // every)).to(F32))
+    assert torch.equal(dbias, (f64(rows).sum(0) * (m // every)).to(F32))
+
+
 def test_a_stage_from_message_to_message():
     """The operators together: a message with its residual is received, normed into 8 bits, multiplied, activated, multiplied back with the
     residual in the epilogue and sent; the gradient's message comes back the other way.  Forward and backward are captured into
