@@ -305,7 +305,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // Tiles in an order that keeps neighbours on one XCD's L2: workgroups go to the eight XCDs in turn, so each XCD takes a run of
-// consecutive tiles, and consecutive tiles are blocks 8 tiles high.
+// consecutive tiles, and consecutive tiles are blocks 8 tiles high (4096 x 14336 x 4096 367 us, 4 high 360, 16 high 395; 4096 x 4096 x
+// 14336 337, 340, 351).
 __device__ __forceinline__ void tile_at(uint32_t id, uint32_t all, uint32_t tm, uint32_t tn, uint32_t &i, uint32_t &j)
 {
     const uint32_t xcd = id & 7, each = all >> 3, more = all & 7;
