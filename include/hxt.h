@@ -545,7 +545,7 @@ int hxt_pack_norm_grad(const hxt_plan_t *plan, const hxt_norm_grad_t *a, void *p
  * work_bytes. */
 typedef enum {
     HXT_ACT_NONE = 0,
-    HXT_ACT_RELU = 1,
+    HXT_ACT_RELU = 1,               /* 0 where z <= 0, minus infinity among it, else z (NaN too); its gradient is 1 where z > 0, else 0 */
     HXT_ACT_GELU = 2,               /* z/2 * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3))) */
     HXT_ACT_SILU = 3                /* z / (1 + exp(-z)) */
 } hxt_act_t;

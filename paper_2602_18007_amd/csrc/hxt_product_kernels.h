@@ -60,7 +60,7 @@ __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf
 constexpr float kGelu2A = 1.5957691216057308f, kGeluB = 0.044715f;
 __device__ __forceinline__ float activate(float z, int act)
 {
-    if (act == HXT_ACT_RELU) return z > 0 ? z : z * 0.0f;               // (0 times NaN stays NaN)
+    if (act == HXT_ACT_RELU) return z <= 0 ? 0.0f : z;                  // (NaN is not <= 0 and stays; minus infinity is)
     if (act == HXT_ACT_SILU) return z * sigmoid(z);
     if (act == HXT_ACT_GELU) return z * sigmoid(kGelu2A * z * (1.0f + kGeluB * z * z));
     return z;
