@@ -166,7 +166,7 @@ int run_product(ProductArgs a, uint8_t *work, size_t work_bytes, hipStream_t st)
     constexpr int64_t es = F == F_E4M3 ? 1 : 2;
     const int64_t m = a.e.m, n = a.e.n, depth = a.p.depth;
     const bool p_direct = vectors(a.p, PA, es), q_direct = vectors(a.q, QA, es);
-    bool direct = p_direct && q_direct;
+    bool direct = (p_direct && q_direct) || depth == 0;       // (of an empty contraction nothing is read, nor copied)
     Shape s = shape_for(m, n, depth, es, !PA && !QA, direct);
     if (!direct) {
         const uint64_t p_bytes = p_direct ? 0 : (PA ? copy_bytes(depth, m, es) : copy_bytes(m, depth, es));

@@ -47,3 +47,46 @@ def test_relu_gradient_at_infinities():
     dz = torch.empty_like(dc)
     hxt.hxt_product_grad(hxt.ProductGrad(dc, pre=pre, act="relu", dz=dz, work=torch.empty(hxt.hxt_product_grad_work_bytes(m, n, 0), dtype=torch.uint8, device=DEV)))
     assert torch.equal(dz.float(), torch.where(pre > 0, dc.float(), torch.zeros(m, n, device=DEV)))
+
+
+@pytest.mark.parametrize("m,n", [(4096, 4096), (3000, 3001), (1024, 14336), (4, 9000), (9, 20000), (64, 14336), (20, 30)])
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_empty_sums_of_any_size(m, n, dtype):
+    """Rows of no elements have a stride of 1 in a tensor and count neither as whole vectors nor as anything to copy."""
+    g = generator(m + n)
+    a, b = torch.empty(m, 0, dtype=dtype, device=DEV), torch.empty(n, 0, dtype=dtype, device=DEV)
+    bias, r = whole((n,), g).to(BF16), whole((m, n), g).to(BF16)
+    want = bias.float() + r.float()
+    assert hxt.hxt_product_work_bytes(m, n, 0, dtype) == 0
+    for work in (None, torch.empty(1 << 20, dtype=torch.uint8, device=DEV)):
+        c = torch.full((m, n), 7.0, dtype=BF16, device=DEV)
+        hxt.hxt_product(hxt.Product(a, b, bias=bias, residual=r, c=c, work=work))
+        assert torch.equal(c.float(), want)
+        plan = hxt.hxt_plan((m, n), None, BF16, 4, 1 << 16)
+        packed, again = (torch.full((plan.packed_bytes,), 0xA5, dtype=torch.uint8, device=DEV) for _ in range(2))
+        sums, want_sums = (torch.empty(plan.num_chunks, dtype=torch.int64, device=DEV) for _ in range(2))
+        hxt.hxt_pack_product(plan, hxt.Product(a, b, bias=bias, residual=r, work=work), packed, sums)
+        hxt.hxt_pack(plan, [c], again, want_sums)
+        assert torch.equal(packed, again) and torch.equal(sums, want_sums)
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("n,k", [(4097, 4097), (4096, 4100), (3001, 3000), (4096, 4096), (14336, 1024)])
+def test_gradients_of_an_empty_micro_batch(n, k, out):
+    """m = 0: the gradients are what was added, of any size."""
+    g = generator(n + k)
+    add, badd = whole((n, k), g).to(out), whole((n,), g)
+    db, dbias = torch.full((n, k), 7.0, dtype=out, device=DEV), torch.full((n,), 7.0, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(torch.empty(0, n, dtype=BF16, device=DEV), torch.empty(0, k, dtype=BF16, device=DEV), db=db, db_add=add,
+                                         dbias=dbias, dbias_add=badd))
+    assert torch.equal(db, add) and torch.equal(dbias, badd)
+    hxt.hxt_product_grad(hxt.ProductGrad(torch.empty(0, n, dtype=BF16, device=DEV), torch.empty(0, k, dtype=BF16, device=DEV), db=db, dbias=dbias))
+    assert bool((db == 0).all()) and bool((dbias == 0).all())
+
+
+@pytest.mark.parametrize("m,k", [(4097, 4097), (4099, 4104), (4096, 4096), (3, 14336)])
+def test_gradient_through_no_columns(m, k):
+    """n = 0: da is 0, of any size."""
+    da = torch.full((m, k), 7.0, dtype=BF16, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(torch.empty(m, 0, dtype=BF16, device=DEV), b=torch.empty(0, k, dtype=BF16, device=DEV), da=da))
+    assert bool((da == 0).all())
