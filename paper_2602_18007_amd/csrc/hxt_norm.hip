@@ -18,7 +18,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm(NormArgs a)
     __shared__ uint32_t part_max[16], part_top[16];
     __shared__ uint64_t parts[SRC == FROM_MESSAGE_SUMMED ? WAVES : 1][4];
     const uint32_t t = threadIdx.x % G, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t first = blockIdx.x * PER, row = first + wave / (G / 64);
+    const uint32_t first = (a.first_group + blockIdx.x) * PER, row = first + wave / (G / 64);
     const bool there = row < a.rows;
     const uint64_t rb = uint64_t(a.cols) * sizeof(T);
     float h[EPT];
@@ -213,11 +213,14 @@ NormArgs norm_args(const hxt_norm_t &a)
 }
 
 template <Source SRC>
-void launch_norm(const NormArgs &n, hxt_dtype_t dtype, hipStream_t st)
+void launch_norm(NormArgs n, hxt_dtype_t dtype, hipStream_t st)
 {
     const RowShape shape = norm_shape(n.rows, n.cols, element_size(dtype));
     const uint32_t per = uint32_t(rows_of(shape));
-    with_shape(dtype, shape, [&]<typename T, int G, int EPT>() { k_norm<T, G, EPT, SRC><<<(n.rows + per - 1) / per, group_threads(shape), 0, st>>>(n); });
+    in_launches((uint64_t(n.rows) + per - 1) / per, uint32_t(group_threads(shape)), [&](uint32_t first, uint32_t count) {
+        n.first_group = first;
+        with_shape(dtype, shape, [&]<typename T, int G, int EPT>() { k_norm<T, G, EPT, SRC><<<count, group_threads(shape), 0, st>>>(n); });
+    });
 }
 
 }  // namespace

@@ -25,6 +25,7 @@ struct Rows {                      // of a tensor
 
 struct NormArgs {
     uint32_t rows, cols;
+    uint32_t first_group;          // number of the launch's first workgroup
     float eps;
     Rows x, residual, h, y, q;     // p == nullptr: not there
     const uint8_t *weight;

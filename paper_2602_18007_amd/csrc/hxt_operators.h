@@ -72,6 +72,16 @@ inline int check_write(const Matrix &m)
     return m.rows > 1 && m.stride < m.cols ? HXT_EINVAL : HXT_OK;
 }
 
+// ---- launches ----------------------------------------------------------------------------
+// HIP takes fewer than 2^32 threads in a launch.  Calls launch(first, count) for `groups` workgroups of that many threads, in as many
+// launches as they need; a run begins at a multiple of 8, so that workgroups go to the same XCDs as in one launch.
+template <typename F>
+inline void in_launches(uint64_t groups, uint32_t threads, F &&launch)
+{
+    const uint64_t most = 0xFFFFFFFFu / threads / 8 * 8;
+    for (uint64_t first = 0; first < groups; first += most) launch(uint32_t(first), uint32_t(groups - first < most ? groups - first : most));
+}
+
 // ---- places in a packed buffer ---------------------------------------------------------
 HXT_HD uint64_t packed_place(const ChunkGeom &g, ChunkAt at)
 {
