@@ -538,7 +538,7 @@ int hxt_pack_norm_grad(const hxt_plan_t *plan, const hxt_norm_grad_t *a, void *p
  * a and b are HXT_BF16, or HXT_E4M3 with a scale for each of their rows (NULL = 1).  c and the residual are out_dtype,
  * HXT_BF16 or, with factors of 16 bits, HXT_F32 (HXT_EUNSUPPORTED: the matrix instruction for 8 bits adds its 128 products with
  * about 20 bits below the largest one, which is enough for a result in bf16 only); pre and bias are HXT_BF16.  m, n or k may be 0 (an empty sum is 0).  residual may be c's
- * matrix.  k <= 2^24, and strides at most 2^22 elements (HXT_EUNSUPPORTED).  work:
+ * matrix.  m and n below 2^31 and of 2^30 tiles of 16 x 16 together, k <= 2^24, and strides at most 2^22 elements (HXT_EUNSUPPORTED).  work:
  * hxt_product_work_bytes bytes or more, 16-byte aligned (HXT_EINVAL if smaller): parts of the sums and, of rows that are no whole
  * 16-byte vectors, copies that are.  (Rows of whole vectors at an odd pitch or base are copied too if the workspace has m * k and
  * n * k elements more, each row rounded up to 16 bytes.)  The order of the sum over k is fixed by m, n, k, the types, the alignment and
@@ -583,7 +583,9 @@ int hxt_pack_product(const hxt_plan_t *plan, const hxt_product_t *a, void *packe
  * dz is rounded to bf16 before it enters the two products (dbias sums it unrounded): both factors of a matrix
  * instruction have 16 bits, and so has every other gradient that crosses layers.  With HXT_ACT_NONE dz is dc: pre is not
  * read, dz is not written and may be NULL.  Otherwise pre and dz are needed; dz may be dc's or pre's matrix.  da, db, dbias may be
- * NULL.  db and db_add are db_dtype (HXT_BF16 or HXT_F32), db_add may be db's matrix, dbias_add may be dbias. */
+ * NULL.  db and db_add are db_dtype (HXT_BF16 or HXT_F32), db_add may be db's matrix, dbias_add may be dbias.  m, n and k are within the
+ * limits of hxt_product in all three products: m and n, over which two of them sum, are 2^24 at most.  work: hxt_product_grad_work_bytes
+ * bytes or more, 16-byte aligned. */
 typedef struct {
     int64_t m, n, k;
     hxt_dtype_t db_dtype;

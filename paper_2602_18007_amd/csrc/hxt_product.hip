@@ -109,6 +109,18 @@ int launched(F &&f)
     return e == hipSuccess ? HXT_OK : operator_fail(e);
 }
 
+// The same for `groups` workgroups of so many threads: launch(arguments, workgroups).
+template <typename F>
+int launched(ProductArgs a, uint64_t groups, uint32_t threads, F &&launch)
+{
+    return launched([&] {
+        in_launches(groups, threads, [&](uint32_t first, uint32_t count) {
+            a.first_group = first;
+            launch(a, count);
+        });
+    });
+}
+
 // A kernel with more than 64 KiB of dynamic LDS says so before it is launched.
 int allow_lds(const void *kernel, uint32_t bytes)
 {
@@ -122,7 +134,9 @@ int launch_tiles(const ProductArgs &a, hipStream_t st)
 {
     constexpr uint32_t lds = product_lds(TM, TN, WM, WN, PA, QA);
     if (const int rc = allow_lds(reinterpret_cast<const void *>(&k_product<F, TM, TN, WM, WN, PA, QA, DIRECT>), lds); rc != HXT_OK) return rc;
-    return launched([&] { k_product<F, TM, TN, WM, WN, PA, QA, DIRECT><<<a.tiles_m * a.tiles_n * a.splits, 64 * WM * WN, lds, st>>>(a); });
+    return launched(a, uint64_t(a.tiles_m) * a.tiles_n * a.splits, 64 * WM * WN, [&](const ProductArgs &run, uint32_t groups) {
+        k_product<F, TM, TN, WM, WN, PA, QA, DIRECT><<<groups, 64 * WM * WN, lds, st>>>(run);
+    });
 }
 
 // A row of 16-byte vectors at 16-byte multiples, in columns too where the rows are the contraction index.
@@ -135,7 +149,7 @@ template <Factor F, int WAVES>
 int launch_rows(const ProductArgs &a, hipStream_t st)
 {
     constexpr uint32_t lds = rows_lds(WAVES);
-    return launched([&] { k_product_rows<F, WAVES><<<up(a.e.n, 16), 64 * WAVES, lds, st>>>(a); });
+    return launched(a, up(a.e.n, 16), 64 * WAVES, [&](const ProductArgs &run, uint32_t groups) { k_product_rows<F, WAVES><<<groups, 64 * WAVES, lds, st>>>(run); });
 }
 
 template <Factor F>
@@ -143,7 +157,7 @@ int launch_ring(const ProductArgs &a, hipStream_t st)
 {
     constexpr uint32_t lds = kRing * 2 * 64 * kStep;
     if (const int rc = allow_lds(reinterpret_cast<const void *>(&k_product_ring<F>), lds); rc != HXT_OK) return rc;
-    return launched([&] { k_product_ring<F><<<a.tiles_m * a.tiles_n * a.splits, 256, lds, st>>>(a); });
+    return launched(a, uint64_t(a.tiles_m) * a.tiles_n * a.splits, 256, [&](const ProductArgs &run, uint32_t groups) { k_product_ring<F><<<groups, 256, lds, st>>>(run); });
 }
 
 // Copies an operand's rows to `to`.
@@ -153,7 +167,11 @@ int align_rows(Operand &o, bool across, uint8_t *to, hipStream_t st)
     using E = std::conditional_t<F == F_E4M3, uint8_t, uint16_t>;
     const uint32_t rows = across ? o.depth : o.rows, cols = across ? o.rows : o.depth, vectors = up(uint64_t(cols) * sizeof(E), 16);
     const uint64_t count = uint64_t(rows) * vectors;
-    const int rc = launched([&] { k_product_align<E><<<up(count, 256), 256, 0, st>>>(o.p, o.stride, cols, count, vectors, reinterpret_cast<u32x4 *>(to)); });
+    const int rc = launched([&] {
+        in_launches((count + 255) / 256, 256, [&](uint32_t first, uint32_t groups) {
+            k_product_align<E><<<groups, 256, 0, st>>>(o.p, o.stride, cols, count, vectors, reinterpret_cast<u32x4 *>(to), first);
+        });
+    });
     o.p = to;
     o.stride = int64_t(vectors) * 16;
     if (across) o.rows = uint32_t(vectors * 16 / sizeof(E));           // (the zeros behind are columns of their own, not stored)

@@ -46,6 +46,7 @@ struct ProductArgs {
     Operand p, q;
     uint32_t tiles_m, tiles_n;
     uint32_t n_first;             // column of the first tile
+    uint32_t first_group;         // number of the launch's first workgroup
     uint32_t splits;              // parts of the contraction; > 1: partial sums go to work[split][m][n]
     uint32_t split_steps;         // steps of one part
     float *work;
@@ -400,10 +401,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs a)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int BUFFER = TileP::BYTES + TileQ::BYTES;
 
-    const uint32_t tiles = a.tiles_m * a.tiles_n;
-    const uint32_t split = a.splits > 1 ? blockIdx.x / tiles : 0;
+    const uint32_t tiles = a.tiles_m * a.tiles_n, group = a.first_group + blockIdx.x;
+    const uint32_t split = a.splits > 1 ? group / tiles : 0;
     uint32_t ti, tj;
-    tile_at(blockIdx.x - split * tiles, tiles, a.tiles_m, a.tiles_n, ti, tj);
+    tile_at(group - split * tiles, tiles, a.tiles_m, a.tiles_n, ti, tj);
     const uint32_t m0 = ti * TM, n0 = a.n_first + tj * TN;
     const int wave = int(threadIdx.x) >> 6, wm = wave / WN, wn = wave % WN;
     const uint32_t depth = a.p.depth, all_steps = (depth + TileP::DEPTH - 1) / TileP::DEPTH;
@@ -570,7 +571,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs a)
         finish_rows<ROUND, COLS, PITCH>(a, split, mine, m0 + wm * ROWS + r0, n0 + wn * COLS);
         __builtin_amdgcn_wave_barrier();
     }
-    if (a.splits <= 1 && a.e.message && blockIdx.x == 0 && !a.n_first) pad_message(a.e);
+    if (a.splits <= 1 && a.e.message && group == 0 && !a.n_first) pad_message(a.e);
 }
 
 // ---- tens of rows -------------------------------------------------------------------------------
@@ -585,7 +586,7 @@ __global__ __launch_bounds__(256) void k_product_ring(ProductArgs a)
     using Tile = TileOf<T, false, ES, 256>;
     constexpr int BUFFER = 2 * Tile::BYTES, LOADS = 2 * Tile::EACH;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const uint32_t tiles = a.tiles_m * a.tiles_n, split = a.splits > 1 ? blockIdx.x / tiles : 0, tile = blockIdx.x - split * tiles;
+    const uint32_t tiles = a.tiles_m * a.tiles_n, group = a.first_group + blockIdx.x, split = a.splits > 1 ? group / tiles : 0, tile = group - split * tiles;
     const uint32_t m0 = tile % a.tiles_m * T, n0 = tile / a.tiles_m * T;
     const int wave = int(threadIdx.x) >> 6, wm = wave >> 1, wn = wave & 1;
     const uint32_t depth = a.p.depth, all_steps = (depth + Tile::DEPTH - 1) / Tile::DEPTH, whole = depth / Tile::DEPTH;
@@ -616,7 +617,7 @@ __global__ __launch_bounds__(256) void k_product_ring(ProductArgs a)
     const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) uint8_t *)lds));
     // workgroups begin at different steps, so that they do not ask the same memory channels at the same time (64 x 14336 x 4096 29.8 ->
     // 27.8 us)
-    const uint32_t begin = steps ? blockIdx.x % steps : 0;
+    const uint32_t begin = steps ? group % steps : 0;
     auto turned = [&](uint32_t s) { return s + begin < steps ? s + begin : s + begin - steps; };
     auto load = [&](uint32_t s) {                            // (past the end the last step again, into a buffer that is not read)
         const uint32_t to = lds0 + s % kRing * BUFFER, step = first + turned(min(s, steps - 1));
@@ -661,7 +662,7 @@ __global__ __launch_bounds__(256) void k_product_ring(ProductArgs a)
         for (int j = 0; j < R; ++j) *reinterpret_cast<f32x4 *>(mine + (16 * i + (l & 15)) * PITCH + 16 * j + 4 * (l >> 4)) = acc[i][j];
     __builtin_amdgcn_wave_barrier();
     finish_rows<32, 32, PITCH>(a, split, mine, m0 + 32 * wm, n0 + 32 * wn);
-    if (a.splits <= 1 && a.e.message && blockIdx.x == 0) pad_message(a.e);
+    if (a.splits <= 1 && a.e.message && group == 0) pad_message(a.e);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
@@ -679,7 +680,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product_rows(ProductArgs a)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     float *parts = reinterpret_cast<float *>(lds);
     const int l = int(threadIdx.x) & 63, r = l & 15, g = l >> 4;
-    const uint32_t wave = threadIdx.x >> 6, n0 = blockIdx.x * 16;
+    const uint32_t wave = threadIdx.x >> 6, n0 = (a.first_group + blockIdx.x) * 16;
     // rows past the end repeat the last one, what comes of them is not stored
     const uint8_t *at_a = a.p.p + int64_t(min(uint32_t(r), a.e.m - 1)) * a.p.stride + 16 * g;
     const uint8_t *at_b = a.q.p + int64_t(min(n0 + r, a.e.n - 1)) * a.q.stride + 16 * g;
@@ -739,7 +740,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product_rows(ProductArgs a)
         }
         finish<8>(a.e, m, n0 + col, z);
     }
-    if (a.e.message && blockIdx.x == 0) pad_message(a.e);
+    if (a.e.message && n0 == 0) pad_message(a.e);
 }
 
 // Sums the parts of a product in their order and finishes it, 4 neighbours a thread.
@@ -772,9 +773,9 @@ __global__ __launch_bounds__(256) void k_product_join(const float *__restrict__ 
 // Rows copied to 16-byte multiples, vectors a row, zeros behind the row's end.
 template <typename E>
 __global__ __launch_bounds__(256) void k_product_align(const uint8_t *__restrict__ from, int64_t stride, uint32_t cols, uint64_t count, uint32_t vectors,
-                                                       u32x4 *__restrict__ to)
+                                                       u32x4 *__restrict__ to, uint32_t first_group)
 {
-    const uint64_t id = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint64_t id = (uint64_t(first_group) + blockIdx.x) * 256 + threadIdx.x;
     if (id >= count) return;
     constexpr uint32_t V = 16 / sizeof(E);
     const uint64_t row = id / vectors;

@@ -90,3 +90,33 @@ def test_gradient_through_no_columns(m, k):
     da = torch.full((m, k), 7.0, dtype=BF16, device=DEV)
     hxt.hxt_product_grad(hxt.ProductGrad(torch.empty(m, 0, dtype=BF16, device=DEV), b=torch.empty(0, k, dtype=BF16, device=DEV), da=da))
     assert bool((da == 0).all())
+
+
+@pytest.mark.parametrize("m", [1, 3])
+def test_more_columns_than_a_launch_has_threads_for(m):
+    """The kernel for few rows has 32 threads a column: of 2^27 columns and more one launch cannot hold them."""
+    n, k = (1 << 27) + 24, 8
+    g = generator(m)
+    a, b = whole((m, k), g).to(BF16), whole((n, k), g).to(BF16)
+    plan = hxt.hxt_plan((m * n,), None, BF16, 4, 64 << 20)
+    packed = torch.full((plan.packed_bytes,), 0xA5, dtype=torch.uint8, device=DEV)
+    sums, got_sums = (torch.empty(plan.num_chunks, dtype=torch.int64, device=DEV) for _ in range(2))
+    hxt.hxt_pack_product(plan, hxt.Product(a, b, work=workspace(m, n, k)), packed, sums)
+    got = torch.empty(m, n, dtype=BF16, device=DEV)
+    hxt.hxt_unpack(plan, packed, [got], got_sums)
+    assert torch.equal(sums, got_sums)
+    for i in range(m):
+        assert torch.equal(got[i], (b.float() * a[i].float()).sum(1).to(BF16))
+
+
+def test_more_copied_vectors_than_a_launch_has_threads_for():
+    """Rows at an odd address are copied to whole vectors first, 16 bytes a thread; here one row stands for 2^23 of 513 vectors."""
+    m, n, k = 1 << 23, 1024, 4104
+    g = generator(9)
+    one, b = whole((k + 1,), g, 1).to(BF16)[1:], whole((n, k), g, 1).to(BF16)
+    room = m * k * 2 + n * k * 2 + (1 << 20)
+    c, work = torch.empty(m, n, dtype=BF16, device=DEV), torch.empty(room, dtype=torch.uint8, device=DEV)
+    hxt.hxt_product(hxt.Product(one.expand(m, k), b, c=c, work=work))
+    want = (b.float() * one.float()).sum(1).to(BF16)
+    for part in c.view(64, -1, n):
+        assert bool((part == want).all())
