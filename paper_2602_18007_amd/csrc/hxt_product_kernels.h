@@ -105,6 +105,14 @@ __device__ __forceinline__ void store_numbers(uint8_t *p, const float *f, bool f
     __builtin_memcpy(p, w, 2 * W);
 }
 
+// z s t, where neither s t nor z s has to lie in binary32's range (hxt_norm's scales go down to 2^-126): the scales' fractions are
+// multiplied, and their exponents added last.  (z is a sum of 8-bit products, 2^-18 at least or 0: z f is exact in its exponent.)
+__device__ __forceinline__ float scaled(float z, float s, float t)
+{
+    const float f = __builtin_amdgcn_frexp_mantf(s) * __builtin_amdgcn_frexp_mantf(t);
+    return __builtin_ldexpf(z * f, __builtin_amdgcn_frexp_expf(s) + __builtin_amdgcn_frexp_expf(t));
+}
+
 // Finishes results (m, n0 .. n0 + W - 1) from their sums.
 template <int W>
 __device__ __forceinline__ void finish(const Epilogue &e, uint32_t m, uint32_t n0, float *z)
@@ -118,7 +126,7 @@ __device__ __forceinline__ void finish(const Epilogue &e, uint32_t m, uint32_t n
             float ns[W];
             if (e.n_scale) __builtin_memcpy(ns, e.n_scale + n0, 4 * W);
 #pragma unroll
-            for (int i = 0; i < W; ++i) z[i] *= e.n_scale ? ms * ns[i] : ms;
+            for (int i = 0; i < W; ++i) z[i] = scaled(z[i], ms, e.n_scale ? ns[i] : 1.0f);
         }
         if (e.bias) {
             float b[W];
@@ -153,7 +161,7 @@ __device__ __forceinline__ void finish(const Epilogue &e, uint32_t m, uint32_t n
         for (int i = 0; i < W; ++i) {
             if (uint32_t(i) >= count) continue;
             const uint32_t n = n0 + i;
-            z[i] *= e.n_scale ? ms * e.n_scale[n] : ms;
+            if (e.m_scale || e.n_scale) z[i] = scaled(z[i], ms, e.n_scale ? e.n_scale[n] : 1.0f);
             if (e.bias) z[i] += bf16_to_f32(e.bias[n]);
             if (e.pre) reinterpret_cast<uint16_t *>(e.pre + m * e.pre_stride)[n] = bf16_of(z[i]);
             z[i] = activate(z[i], e.act);

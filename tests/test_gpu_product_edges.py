@@ -120,3 +120,23 @@ def test_more_copied_vectors_than_a_launch_has_threads_for():
     want = (b.float() * one.float()).sum(1).to(BF16)
     for part in c.view(64, -1, n):
         assert bool((part == want).all())
+
+
+@pytest.mark.parametrize("m,n,k", WAYS)
+def test_scales_whose_product_leaves_binary32(m, n, k):
+    """A row's scale may be 2^-126 (hxt_norm's least): times a column's 2^-19 it would be subnormal, with a few bits left, though sums are
+    2^22 and more here; two large ones would be infinite, and a sum of 0 NaN.  Every step in front of the rounding to bf16 is off by
+    2^-24 of its value at most, the results by 2^-8 and 3 of those."""
+    g = generator(m * n + k)
+    a, b = ((torch.randint(8, 15, (r, k), generator=g, device=DEV) * 32).float().to(E4M3) for r in (m, n))      # 256 .. 448
+    a.view(torch.uint8)[2], b.view(torch.uint8)[1] = 0, 0
+    sa = (torch.rand(m, generator=g, device=DEV) + 1) * 2.0 ** -126
+    sb = (torch.rand(n, generator=g, device=DEV) + 1) * 2.0 ** -19
+    sa[1], sa[2], sb[1] = 2.0 ** 100, 2.0 ** 100, 2.0 ** 40
+    c = torch.empty(m, n, dtype=BF16, device=DEV)
+    hxt.hxt_product(hxt.Product(a, b, a_scale=sa, b_scale=sb, c=c, work=workspace(m, n, k, E4M3)))
+    sums = f64(a) @ f64(b).t().contiguous()
+    want = sums * f64(sa)[:, None] * f64(sb)
+    # the matrix instruction for 8 bits adds 128 products with 20 bits below the largest; results below 2^-126 have steps of 2^-133
+    within(c, want, want.abs() * (HALF[BF16] + 2.0 ** -13 + (k + 4) * 2.0 ** -24 + 3 * 2.0 ** -24) + 2.0 ** -134, "c")
+    assert bool((c[2] == 0).all()) and bool((c[:, 1] == 0).all())
