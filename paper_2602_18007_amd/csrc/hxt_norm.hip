@@ -9,7 +9,7 @@ namespace {
 // ---- forward --------------------------------------------------------------------------
 // Each row belongs to G threads, EPT values each, read once: x (of a message through its chunks) plus the residual as binary32,
 // then the sum of squares, then the outputs, of q after one more total.  Bound by memory: a 4096 x 4096 message of x and residual
-// into h and 8 bits with its sums 24.8 us (117 MB, 4.7 TB/s), 8192 x 3584 with a residual into h and y 46.3 us (235 MB, 5.1 TB/s).
+// into h and 8 bits with its sums 25.3 us (117 MB, 4.6 TB/s), 8192 x 3584 with a residual into h and y 46.3 us (235 MB, 5.1 TB/s).
 template <typename T, int G, int EPT, Source SRC>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm(NormArgs a)
 {
@@ -114,10 +114,22 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm(NormArgs a)
     }
     if (a.q.p) {
         top = row_max<G>(top, part_max);
-        // A row's largest value becomes 448.  (A tiny row's scale stays a normal number, whose reciprocal is one too.)
+        // A row's largest value becomes 448.
         const float scale = top > 0x7F800000u ? __uint_as_float(0x7FC00000u) : fmaxf(__uint_as_float(top) / kE4m3Max, kLeastScale);
-        const float inverse = 1.0f / scale;
         if (there && t == 0) a.scale[row] = scale;
+        // y / scale as binary32 rounds it: the product with 1 / scale, put right by what it leaves.  Tiny rows are lifted first, so that
+        // this is a normal number; of an infinite scale nothing is taken away (finite values are 0 in it, infinite ones NaN).  (4096 x
+        // 4096 with a residual: 25.3 us, with the product alone 24.8.)
+        const bool tiny = scale < 0x1p-60f;               // (a row's threads are whole waves)
+        const float unit = tiny ? scale * 0x1p64f : scale, inverse = 1.0f / unit, taken = unit < INFINITY ? unit : 0.0f;
+        if (tiny) {
+#pragma unroll
+            for (int i = 0; i < EPT; ++i) h[i] *= 0x1p64f;
+        }
+        auto quotient = [&](float v) {
+            const float about = v * inverse;
+            return fmaf(fmaf(-about, taken, v), inverse, about);
+        };
 #pragma unroll
         for (uint32_t i = 0; i < NV; ++i) {
             const uint32_t v = i * G + t, n = there && v * V < a.cols ? min(V, a.cols - v * V) : 0;
@@ -126,7 +138,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm(NormArgs a)
             uint8_t *to = a.q.row(row) + size_t(v) * V;
             uint32_t w[V / 4];
 #pragma unroll
-            for (uint32_t j = 0; j < V; j += 4) w[j / 4] = e4m3x4(f[j] * inverse, f[j + 1] * inverse, f[j + 2] * inverse, f[j + 3] * inverse);
+            for (uint32_t j = 0; j < V; j += 4) w[j / 4] = e4m3x4(quotient(f[j]), quotient(f[j + 1]), quotient(f[j + 2]), quotient(f[j + 3]));
             if (n == V) {
                 if constexpr (V == 8) {
                     if (a.nt) __builtin_nontemporal_store(u32x2{w[0], w[1]}, reinterpret_cast<u32x2_any *>(to));

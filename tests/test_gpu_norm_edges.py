@@ -45,3 +45,35 @@ def test_more_rows_of_a_message_than_a_launch_has_threads_for():
         X = f64(x[at])
         Y = X / torch.sqrt((X * X).mean(1, keepdim=True) + EPS)
         within(y[at], Y, Y.abs() * (HALF[BF16] + EPS32) + SMALLEST[BF16], "y")
+
+
+@pytest.mark.parametrize("std", [1.0, 1e-3])
+@pytest.mark.parametrize("rows,cols", [(4096, 4096), (1000, 8000), (60000, 200), (2, 32768)])
+def test_eight_bits_are_the_quotient_rounded(rows, cols, std):
+    """q is y / scale, that quotient in binary32 and then to nearest even: of f32 rows y is the very value that is divided.  Among millions
+    of values some lie so close to the middle of two steps that the product with 1 / scale falls on its other side."""
+    g = generator(rows + cols)
+    x, w = normal((rows, cols), g, 2.0), 1 + 0.2 * normal((cols,), g)
+    w *= std
+    y, q, scale = torch.empty_like(x), torch.empty(rows, cols, dtype=E4M3, device=DEV), torch.empty(rows, device=DEV)
+    hxt.hxt_norm(hxt.Norm(w, EPS, x=x, y=y, q=q, scale=scale))
+    want = (y.cpu() / scale.cpu()[:, None]).to(E4M3)
+    assert int((q.cpu().float() != want.float()).sum()) == 0
+
+
+def test_eight_bits_at_the_middle_of_two_steps():
+    """Rows whose values are odd multiples of half a step times a scale that is no power of two, from the smallest scales to the largest:
+    the quotient is exact or one binary32 step off the middle, and goes where that quotient goes."""
+    cols = 256
+    grid = torch.arange(1, cols, device=DEV).float() * 0.5 + 8                      # 8.5 .. 135.5: middles among them
+    rows = []
+    for e in list(range(-130, 110, 7)):
+        for f in (1.0, 1.1, 1.3333334, 1.7, 1.9999999):
+            rows.append(torch.cat([grid * 2, torch.tensor([448.0], device=DEV)]).double() * f * 2.0 ** e)
+    w = torch.stack(rows).to(F32)
+    x = torch.ones(1, cols, device=DEV)
+    y, q, scale = torch.empty_like(x), torch.empty(1, cols, dtype=E4M3, device=DEV), torch.empty(1, device=DEV)
+    for weight in w:
+        hxt.hxt_norm(hxt.Norm(weight.contiguous(), 1e-24, x=x, y=y, q=q, scale=scale))
+        want = (y.cpu() / scale.cpu()).to(E4M3)
+        assert int((q.cpu().float() != want.float()).sum()) == 0, scale.item()
