@@ -535,7 +535,8 @@ int hxt_pack_norm_grad(const hxt_plan_t *plan, const hxt_norm_grad_t *a, void *p
 
 /* Matrix product of a [m, k] and the rows of b [n, k] (as a linear layer keeps its weight), with its epilogue:
  *     z = sum_k a * b  [* a_scale[m] * b_scale[n]]  [+ bias[n]],   pre = z,   c = act(z) [+ residual]
- * a and b are HXT_BF16, or HXT_E4M3 with a scale for each of their rows (NULL = 1).  c and the residual are out_dtype,
+ * a and b are HXT_BF16, or HXT_E4M3 with a scale for each of their rows (NULL = 1; a_scale any, b_scale 0 or of 2^-100 .. 2^80, beyond
+ * which results may lose their bits or overflow on the way).  c and the residual are out_dtype,
  * HXT_BF16 or, with factors of 16 bits, HXT_F32 (HXT_EUNSUPPORTED: the matrix instruction for 8 bits adds its 128 products with
  * about 20 bits below the largest one, which is enough for a result in bf16 only); pre and bias are HXT_BF16.  m, n or k may be 0 (an empty sum is 0).  residual may be c's
  * matrix.  m and n below 2^31 and of 2^30 tiles of 16 x 16 together, k <= 2^24, and strides at most 2^22 elements (HXT_EUNSUPPORTED).  work:

@@ -105,12 +105,11 @@ __device__ __forceinline__ void store_numbers(uint8_t *p, const float *f, bool f
     __builtin_memcpy(p, w, 2 * W);
 }
 
-// z s t, where neither s t nor z s has to lie in binary32's range (hxt_norm's scales go down to 2^-126): the scales' fractions are
-// multiplied, and their exponents added last.  (z is a sum of 8-bit products, 2^-18 at least or 0: z f is exact in its exponent.)
+// z * s * t, where neither s * t nor z * s has to lie in binary32's range (hxt_norm's scales go down to 2^-126): s's exponent is added
+// last.  (A sum of 8-bit products is 0 or between 2^-18 and 2^42.)
 __device__ __forceinline__ float scaled(float z, float s, float t)
 {
-    const float f = __builtin_amdgcn_frexp_mantf(s) * __builtin_amdgcn_frexp_mantf(t);
-    return __builtin_ldexpf(z * f, __builtin_amdgcn_frexp_expf(s) + __builtin_amdgcn_frexp_expf(t));
+    return __builtin_ldexpf(z * (__builtin_amdgcn_frexp_mantf(s) * t), __builtin_amdgcn_frexp_expf(s));
 }
 
 // Finishes results (m, n0 .. n0 + W - 1) from their sums.
