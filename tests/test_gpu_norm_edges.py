@@ -77,3 +77,27 @@ def test_eight_bits_at_the_middle_of_two_steps():
         hxt.hxt_norm(hxt.Norm(weight.contiguous(), 1e-24, x=x, y=y, q=q, scale=scale))
         want = (y.cpu() / scale.cpu()).to(E4M3)
         assert int((q.cpu().float() != want.float()).sum()) == 0, scale.item()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", [(3, 64), (5, 1000), (3, 4096), (3, 8200), (1031, 520), (1025, 3000), (1024, 20008)])
+def test_eight_bits_of_rows_with_an_infinite_scale(rows, cols, dtype):
+    """An infinite weight gives values and so a scale of infinity: what is finite is 0 in units of it, what is infinite NaN.  A row with 0
+    in that place has a NaN in y, and a scale of NaN."""
+    g = generator(rows * 5 + cols)
+    x, w = normal((rows, cols), g, 1.0, dtype), (1 + 0.2 * normal((cols,), g)).to(dtype)
+    bad = cols // 3
+    w[bad] = float("inf")
+    x[:, bad] = 1.5
+    x[1, bad] = 0
+    x[2, bad] = -2.0
+    y, q, scale = torch.empty_like(x), torch.empty(rows, cols, dtype=E4M3, device=DEV), torch.full((rows,), -1.0, device=DEV)
+    hxt.hxt_norm(hxt.Norm(w, EPS, x=x, y=y, q=q, scale=scale))
+    y, q = y.float(), q.float()
+    others = [i for i in range(rows) if i != 1]
+    assert bool(torch.isinf(y[others, bad]).all()) and y[2, bad].item() == -float("inf") and bool(torch.isnan(y[1, bad]))
+    assert bool((scale[others] == float("inf")).all()) and bool(torch.isnan(scale[1]))
+    assert bool(torch.isnan(q[others, bad]).all()) and bool(torch.isnan(q[1]).all())
+    rest = torch.ones(cols, dtype=torch.bool, device=DEV)
+    rest[bad] = False
+    assert bool((q[others][:, rest] == 0).all()) and bool(torch.isfinite(y[others][:, rest]).all())

@@ -1,0 +1,26 @@
+"""What the operators at the ends of a stage take and refuse at an edge, through the C ABI and the binding, on the CPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2602_18007_amd import hxt
+from tests.test_operator_refusals import BF16, E4M3, F32, NO_GPU, at, product_block, status
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(40, 1000, 4160, hxt.HXT_BF16), (60, 2000, 4224, hxt.HXT_E4M3), (130, 520, 8201, hxt.HXT_BF16)])
+def test_product_refuses_a_workspace_that_is_missing_small_or_misplaced(m, n, k, dtype):
+    need = hxt.lib().hxt_product_work_bytes(m, n, k, dtype)
+    assert need > 4096
+    kw = dict(m=m, n=n, k=k, dtype=dtype, a_stride=k, b_stride=k, residual_stride=n, pre_stride=n, c_stride=n)
+    assert status("hxt_product", product_block(**kw)) == hxt.HXT_EINVAL
+    assert status("hxt_product", product_block(work=at(7), work_bytes=need - 1, **kw)) == hxt.HXT_EINVAL
+    assert status("hxt_product", product_block(work=None, work_bytes=need, **kw)) == hxt.HXT_EINVAL
+    assert status("hxt_product", product_block(work=at(7) + 4, work_bytes=need, **kw)) == hxt.HXT_EALIGN
+    for other in (0, 1, 2, 3, 4, 5):                     # a, b, bias, residual, pre, c
+        assert status("hxt_product", product_block(work=at(other), work_bytes=need, **kw)) == hxt.HXT_EOVERLAP
+    plan = hxt.hxt_plan((m, n), None, BF16, 2, 4096)
+    kw.pop("c_stride")
+    for work, size in ((None, 0), (at(7), need - 1)):
+        block = product_block(c=None, work=work, work_bytes=size, **kw)
+        assert hxt.lib().hxt_pack_product(plan.handle, C.byref(block), at(9), None, None) == hxt.HXT_EINVAL
