@@ -94,13 +94,15 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm_grad(NormGradArgs a)
         };
         const float rstd = reciprocal_rms<G, EPT>(ss, [&](int i) { return element(h, i); }, a.cols, a.eps, part_s, part_top);
         float mean = sg * rstd / float(a.cols);                 // of g * n
-        if (any_row<G>(ss > kSquaresLeave)) {
+        // Where the sum of squares or this one has left binary32's range: once more, from the normed row.
+        const bool left = ss > kSquaresLeave || !(fabsf(sg) <= kSquaresLeave);
+        if (any_row<G>(left)) {
             float s = 0;
 #pragma unroll
             for (int i = 0; i < EPT; ++i) s += element(h, i) * rstd * (element(dy, i) * element(w, i));
             if constexpr (G > 64) __syncthreads();
             s = row_sum<G>(s, part_g);
-            if (ss > kSquaresLeave) mean = s / float(a.cols);
+            if (left) mean = s / float(a.cols);
         }
         // (widened again, not kept from the sums: that would be twice the registers)
 #pragma unroll

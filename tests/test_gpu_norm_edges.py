@@ -101,3 +101,23 @@ def test_eight_bits_of_rows_with_an_infinite_scale(rows, cols, dtype):
     rest = torch.ones(cols, dtype=torch.bool, device=DEV)
     rest[bad] = False
     assert bool((q[others][:, rest] == 0).all()) and bool(torch.isfinite(y[others][:, rest]).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", [(5, 300), (6, 1000), (5, 4096), (4, 8192), (3, 16384), (3, 20000)])
+def test_gradient_of_rows_whose_products_leave_binary32(rows, cols, dtype):
+    """h^2 stays inside binary32 and h dy w does not: the gradient is of dy's size over h's, a number like any other."""
+    g = generator(rows * 7 + cols)
+    h, dy, dh = (normal((rows, cols), g, s, F32) for s in (1.0, 1.0, 0.1))
+    h[0] *= 1e13
+    dy[0] *= 1e30
+    h[1] *= 1e16
+    dy[1] *= 1e24
+    h, dy, dh = h.to(dtype), dy.to(dtype), dh.to(dtype)
+    w = (1 + 0.2 * normal((cols,), g)).to(dtype)
+    dx, dweight = torch.empty_like(h), torch.empty(cols, device=DEV)
+    work = torch.empty(hxt.hxt_norm_grad_work_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    hxt.hxt_norm_grad(hxt.NormGrad(w, EPS, h=h, dy=dy, dh=dh, dx=dx, dweight=dweight, work=work))
+    DX, size, DW, dw_size = norm_grad_exact(h, dy, dh, w, EPS)
+    within(dx, DX, DX.abs() * (HALF[dtype] + 2.0 ** -24) + size * 4 * EPS32 + SMALLEST[dtype], "dx")
+    within(dweight, DW, dw_size * (200 * 2.0 ** -24 + 2 * EPS32) + DW.abs() * 2.0 ** -23, "dweight")
