@@ -181,7 +181,7 @@ int check_norm(const hxt_norm_t *a, bool message)
     if (!a) return HXT_EINVAL;
     int rc = check_sizes(a->rows, a->cols, a->dtype, a->eps);
     if (rc != HXT_OK) return rc;
-    if ((!a->h && !a->y && !a->q) || (a->q && !a->scale)) return HXT_EINVAL;
+    if ((!a->h && !a->y && !a->q && a->rows > 0) || (a->q && !a->scale)) return HXT_EINVAL;
     if (message ? a->x != nullptr : (!a->x && a->rows > 0)) return HXT_EINVAL;
     const Norm m(*a);
     for (const Matrix *r : {&m.x, &m.residual})

@@ -24,3 +24,25 @@ def test_product_refuses_a_workspace_that_is_missing_small_or_misplaced(m, n, k,
     for work, size in ((None, 0), (at(7), need - 1)):
         block = product_block(c=None, work=work, work_bytes=size, **kw)
         assert hxt.lib().hxt_pack_product(plan.handle, C.byref(block), at(9), None, None) == hxt.HXT_EINVAL
+
+
+def test_norms_of_no_rows_through_the_binding():
+    """A tensor without elements has no address: that its rows are none is no missing output."""
+    dev = "cuda:0" if torch.cuda.is_available() else "cpu"
+    for dt in (BF16, F32):
+        e, q, s = torch.empty(0, 64, dtype=dt, device=dev), torch.empty(0, 64, dtype=E4M3, device=dev), torch.empty(0, device=dev)
+        w = torch.ones(64, dtype=dt, device=dev)
+        hxt.hxt_norm(hxt.Norm(w, x=e, y=e))
+        hxt.hxt_norm(hxt.Norm(w, x=e, residual=e, h=e, y=e, q=q, scale=s))
+        hxt.hxt_norm(hxt.Norm(w, x=e, q=q, scale=s))
+    b = hxt._Norm(rows=0, cols=64, dtype=hxt.HXT_BF16, eps=1e-5)
+    assert status("hxt_norm", b) == hxt.HXT_OK
+    b.rows, b.x, b.x_stride = 1, at(0), 64
+    assert status("hxt_norm", b) == hxt.HXT_EINVAL       # (with rows an output is needed)
+
+
+def test_message_norm_of_no_rows():
+    plan = hxt.hxt_plan((0, 64), None, BF16, 2, 256)
+    assert plan.num_chunks == 0
+    b = hxt._Norm(rows=0, cols=64, dtype=hxt.HXT_BF16, eps=1e-5)
+    assert hxt.lib().hxt_unpack_norm(plan.handle, None, C.byref(b), None, None) == hxt.HXT_OK
