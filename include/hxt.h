@@ -539,7 +539,7 @@ int hxt_pack_norm_grad(const hxt_plan_t *plan, const hxt_norm_grad_t *a, void *p
  * which results may lose their bits or overflow on the way).  c and the residual are out_dtype,
  * HXT_BF16 or, with factors of 16 bits, HXT_F32 (HXT_EUNSUPPORTED: the matrix instruction for 8 bits adds its 128 products with
  * about 20 bits below the largest one, which is enough for a result in bf16 only); pre and bias are HXT_BF16.  m, n or k may be 0 (an empty sum is 0).  residual may be c's
- * matrix.  m and n below 2^31 and of 2^30 tiles of 16 x 16 together, k <= 2^24, and strides at most 2^22 elements (HXT_EUNSUPPORTED).  work:
+ * matrix.  m and n below 2^31 and of 2^30 tiles of 16 x 16 together, k <= 2^24, and strides, of more than one row, at most 2^22 elements (HXT_EUNSUPPORTED).  work:
  * hxt_product_work_bytes bytes or more, 16-byte aligned (HXT_EINVAL if smaller): parts of the sums and, of rows that are no whole
  * 16-byte vectors, copies that are.  (Rows of whole vectors at an odd pitch or base are copied too if the workspace has m * k and
  * n * k elements more, each row rounded up to 16 bytes.)  The order of the sum over k is fixed by m, n, k, the types, the alignment and

@@ -225,16 +225,14 @@ int run_product(ProductArgs a, uint8_t *work, size_t work_bytes, hipStream_t st)
     return launched([&] { k_product_join<<<up(groups, 256), 256, 0, st>>>(a.work, a.splits, a.e); });
 }
 
+// One row's stride is no distance between rows: any is taken, and only whether it is a whole number of vectors is kept, by
+// which a way is chosen.
+bool far(const Matrix &m) { return !m.none() && m.rows > 1 && m.stride > kMostStride; }
+int64_t row_stride(const Matrix &m) { return (m.rows > 1 ? m.stride : m.stride % 16) * m.es; }
+
 Operand operand(const Matrix &m, bool across)
 {
-    return Operand{reinterpret_cast<const uint8_t *>(m.p), int64_t(m.pitch()), uint32_t(across ? m.cols : m.rows), uint32_t(across ? m.rows : m.cols)};
-}
-
-Operand operand_read(const Matrix &m, bool across)       // a read matrix's stride counts also where it has one row
-{
-    Operand o = operand(m, across);
-    o.stride = m.stride * m.es;
-    return o;
+    return Operand{reinterpret_cast<const uint8_t *>(m.p), row_stride(m), uint32_t(across ? m.cols : m.rows), uint32_t(across ? m.rows : m.cols)};
 }
 
 // ---- forward --------------------------------------------------------------------------------
@@ -272,11 +270,11 @@ int check_product(const hxt_product_t *x, bool message)
     const Product p(*x);
     for (const Matrix *r : {&p.a, &p.b, &p.residual}) {
         if ((rc = check_read(*r)) != HXT_OK) return rc;
-        if (!r->none() && r->stride > kMostStride) return HXT_EUNSUPPORTED;
+        if (far(*r)) return HXT_EUNSUPPORTED;
     }
     for (const Matrix *w : {&p.pre, &p.c}) {
         if ((rc = check_write(*w)) != HXT_OK) return rc;
-        if (!w->none() && w->stride > kMostStride) return HXT_EUNSUPPORTED;
+        if (far(*w)) return HXT_EUNSUPPORTED;
     }
     for (const Matrix *r : {&p.a_scale, &p.b_scale, &p.bias})
         if ((rc = check_read(*r)) != HXT_OK) return rc;
@@ -296,8 +294,8 @@ int launch_forward(const hxt_product_t &x, const Plan *plan, void *packed, hipSt
     const Product p(x);
     ProductArgs a;
     std::memset(&a, 0, sizeof a);
-    a.p = operand_read(p.a, false);
-    a.q = operand_read(p.b, false);
+    a.p = operand(p.a, false);
+    a.q = operand(p.b, false);
     Epilogue &e = a.e;
     e.m = uint32_t(x.m);
     e.n = uint32_t(x.n);
@@ -306,7 +304,7 @@ int launch_forward(const hxt_product_t &x, const Plan *plan, void *packed, hipSt
     e.bias = static_cast<const uint16_t *>(x.bias);
     e.act = x.act;
     e.residual = static_cast<const uint8_t *>(x.residual);
-    e.residual_stride = x.residual_stride * p.residual.es;
+    e.residual_stride = row_stride(p.residual);
     e.pre = static_cast<uint8_t *>(x.pre);
     e.pre_stride = int64_t(p.pre.pitch());
     e.out = static_cast<uint8_t *>(plan ? packed : x.c);
@@ -353,11 +351,11 @@ int check_product_grad(const hxt_product_grad_t *x)
     const ProductGrad p(*x);
     for (const Matrix *r : {&p.dc, &p.pre, &p.a, &p.b, &p.db_add}) {
         if ((rc = check_read(*r)) != HXT_OK) return rc;
-        if (!r->none() && r->stride > kMostStride) return HXT_EUNSUPPORTED;
+        if (far(*r)) return HXT_EUNSUPPORTED;
     }
     for (const Matrix *w : {&p.dz, &p.da, &p.db}) {
         if ((rc = check_write(*w)) != HXT_OK) return rc;
-        if (!w->none() && w->stride > kMostStride) return HXT_EUNSUPPORTED;
+        if (far(*w)) return HXT_EUNSUPPORTED;
     }
     for (const Matrix *r : {&p.dbias, &p.dbias_add})
         if ((rc = check_read(*r)) != HXT_OK) return rc;
@@ -404,8 +402,8 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
         d.n = uint32_t(x.n);
         d.dc = static_cast<const uint8_t *>(x.dc);
         d.pre = static_cast<const uint8_t *>(x.pre);
-        d.dc_stride = x.dc_stride * 2;
-        d.pre_stride = x.pre_stride * 2;
+        d.dc_stride = row_stride(p.dc);
+        d.pre_stride = row_stride(p.pre);
         d.dz = copies ? static_cast<uint8_t *>(x.dz) : nullptr;
         d.dz_stride = int64_t(p.dz.pitch());
         d.act = x.act;
@@ -420,8 +418,8 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
     if (x.da && x.m > 0 && x.k > 0) {
         ProductArgs a;
         std::memset(&a, 0, sizeof a);
-        a.p = operand_read(dz, false);
-        a.q = operand_read(p.b, true);
+        a.p = operand(dz, false);
+        a.q = operand(p.b, true);
         a.p.depth = a.q.depth = uint32_t(x.n);
         a.e = plain(p.da, false);
         if ((rc = run_product<F_BF16, false, true>(a, work, room, st)) != HXT_OK) return rc;
@@ -429,12 +427,12 @@ int launch_grad(const hxt_product_grad_t &x, hipStream_t st)
     if (x.db && x.n > 0 && x.k > 0) {
         ProductArgs a;
         std::memset(&a, 0, sizeof a);
-        a.p = operand_read(dz, true);
-        a.q = operand_read(p.a, true);
+        a.p = operand(dz, true);
+        a.q = operand(p.a, true);
         a.p.depth = a.q.depth = uint32_t(x.m);
         a.e = plain(p.db, x.db_dtype == HXT_F32);
         a.e.residual = reinterpret_cast<const uint8_t *>(p.db_add.p);
-        a.e.residual_stride = x.db_add_stride * p.db_add.es;
+        a.e.residual_stride = row_stride(p.db_add);
         if ((rc = run_product<F_BF16, true, true>(a, work, room, st)) != HXT_OK) return rc;
     }
     return HXT_OK;

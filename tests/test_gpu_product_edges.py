@@ -140,3 +140,31 @@ def test_scales_whose_product_leaves_binary32(m, n, k):
     # the matrix instruction for 8 bits adds 128 products with 20 bits below the largest; results below 2^-126 have steps of 2^-133
     within(c, want, want.abs() * (HALF[BF16] + 2.0 ** -13 + (k + 4) * 2.0 ** -24 + 3 * 2.0 ** -24) + 2.0 ** -134, "c")
     assert bool((c[2] == 0).all()) and bool((c[:, 1] == 0).all())
+
+
+def test_long_single_rows():
+    """One row of a result, of a gradient or of a factor may be longer than the distance that rows may have."""
+    n, k = (1 << 22) + 24, 40
+    g = generator(11)
+    a, b, bias = whole((1, k), g).to(BF16), whole((n, k), g).to(BF16), whole((n,), g).to(BF16)
+    pre, c, r = torch.empty(1, n, dtype=BF16, device=DEV), torch.empty(1, n, dtype=BF16, device=DEV), whole((1, n), g).to(BF16)
+    hxt.hxt_product(hxt.Product(a, b, bias=bias, act="relu", pre=pre, residual=r, c=c, work=workspace(1, n, k)))
+    z = (b.float() * a.float()).sum(1) + bias.float()
+    assert torch.equal(pre[0], z.to(BF16)) and torch.equal(c[0], (torch.relu(z) + r[0].float()).to(BF16))
+    dc = whole((1, n), g).to(BF16)
+    dz, da, db, dbias = torch.empty_like(dc), torch.empty_like(a), torch.empty_like(b), torch.empty(n, device=DEV)
+    work = torch.empty(hxt.hxt_product_grad_work_bytes(1, n, k), dtype=torch.uint8, device=DEV)
+    hxt.hxt_product_grad(hxt.ProductGrad(dc, a, b, pre=pre, act="relu", dz=dz, da=da, db=db, dbias=dbias, work=work))
+    d = torch.where(pre > 0, dc.float(), torch.zeros_like(dc, dtype=F32))
+    assert torch.equal(dz.float(), d) and torch.equal(dbias, d[0]) and torch.equal(db, (d[0][:, None] * a.float()).to(BF16))
+    assert torch.equal(da, (f64(d) @ f64(b)).to(F32).to(BF16))
+    long = (1 << 22) + 72
+    x, y = whole((1, long), g, 1).to(BF16), whole((1, long), g, 1).to(BF16)
+    one = torch.empty(1, 1, device=DEV)
+    hxt.hxt_product(hxt.Product(x, y, c=one, out_dtype=F32, work=workspace(1, 1, long)))
+    assert one.item() == (f64(x) * f64(y)).sum().item()
+    spread = torch.zeros(1, 3, (1 << 23) + 8, dtype=BF16, device=DEV)[:, 1:2, :k]      # (a stride of 2^23 + 8)
+    spread.copy_(a)
+    out = torch.empty(1, 1, n, dtype=BF16, device=DEV)
+    hxt.hxt_product(hxt.Product(spread, b, bias=bias, c=out, work=workspace(1, n, k)))
+    assert torch.equal(out.view(-1), z.to(BF16))

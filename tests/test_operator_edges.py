@@ -46,3 +46,27 @@ def test_message_norm_of_no_rows():
     assert plan.num_chunks == 0
     b = hxt._Norm(rows=0, cols=64, dtype=hxt.HXT_BF16, eps=1e-5)
     assert hxt.lib().hxt_unpack_norm(plan.handle, None, C.byref(b), None, None) == hxt.HXT_OK
+
+
+@NO_GPU
+@pytest.mark.parametrize("change", [
+    dict(m=1, n=(1 << 22) + 8, k=64, a_stride=64, b_stride=64, residual_stride=(1 << 22) + 8, pre_stride=(1 << 22) + 8, c_stride=(1 << 22) + 8, bias=None),
+    dict(m=1, a_stride=1 << 40, residual_stride=1 << 62, pre_stride=0, c_stride=1 << 40),
+    dict(n=1, k=64, b_stride=1 << 40, residual_stride=1, pre_stride=1, c_stride=1),
+    dict(m=1, n=1, k=(1 << 22) + 64, a=at(0), a_stride=(1 << 22) + 64, b_stride=(1 << 22) + 64, work=at(7), work_bytes=1 << 20),
+])
+def test_one_row_has_no_stride_to_speak_of(change):
+    """A [1, n] tensor's row stride is n or anything else: it is no distance between rows.  (Addresses here are 2^28 apart.)"""
+    assert status("hxt_product", product_block(**change)) == hxt.HXT_EHIP
+
+
+@NO_GPU
+def test_one_row_of_a_gradient_has_no_stride_to_speak_of():
+    n = (1 << 22) + 8
+    b = hxt._ProductGrad(m=1, n=n, k=8, db_dtype=hxt.HXT_BF16, act=2, dc=at(0), dc_stride=n, pre=at(1), pre_stride=1 << 50, a=at(2), a_stride=1 << 41, b=at(3),
+                         b_stride=8, dz=at(4), dz_stride=n, da=at(5), da_stride=1 << 60, db=at(6), db_stride=8, work=at(8), work_bytes=1 << 27)
+    assert status("hxt_product_grad", b) == hxt.HXT_EHIP
+    b.m = 2
+    assert status("hxt_product_grad", b) == hxt.HXT_EUNSUPPORTED
+    b.m, b.dc_stride = 1, -1
+    assert status("hxt_product_grad", b) == hxt.HXT_EINVAL
