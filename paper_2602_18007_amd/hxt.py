@@ -10,6 +10,7 @@ PyTorch is used for device memory and streams only.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional, Sequence
 
@@ -540,7 +541,7 @@ class _Arguments:
             return
         if t.dtype != dtype:
             raise ValueError("%s is %s, not %s" % (name, t.dtype, dtype))
-        v = t if t.dim() == 2 else t.reshape(1, 1) if t.dim() == 0 else t.unsqueeze(0) if t.dim() == 1 else t.view(-1, t.shape[-1])
+        v = t if t.dim() == 2 else t.reshape(1, 1) if t.dim() == 0 else t.unsqueeze(0) if t.dim() == 1 else t.view(*_shape_of([t]))
         if tuple(v.shape) != (rows, cols):
             raise ValueError("%s is %s, not rows of [%d, %d]" % (name, tuple(t.shape), rows, cols))
         if cols > 1 and v.stride(1) != 1 and v.numel():
@@ -576,8 +577,7 @@ class _Arguments:
 def _shape_of(named):
     for t in named:
         if t is not None:
-            cols = t.shape[-1] if t.dim() else 1
-            return (t.numel() // cols if cols else (t.shape[0] if t.dim() == 2 else 0)), cols
+            return math.prod(t.shape[:-1]), t.shape[-1] if t.dim() else 1
     raise ValueError("no tensor says how many rows there are")
 
 

@@ -70,3 +70,16 @@ def test_one_row_of_a_gradient_has_no_stride_to_speak_of():
     assert status("hxt_product_grad", b) == hxt.HXT_EUNSUPPORTED
     b.m, b.dc_stride = 1, -1
     assert status("hxt_product_grad", b) == hxt.HXT_EINVAL
+
+
+def test_the_binding_takes_rows_of_no_elements():
+    """An empty contraction of [batch, seq, 0] factors, and no rows of [0, seq, n]."""
+    a, b = torch.empty(2, 3, 0, dtype=BF16), torch.empty(5, 0, dtype=BF16)
+    p = hxt.Product(a, b, c=torch.empty(2, 3, 5, dtype=BF16))
+    assert (p.c.m, p.c.n, p.c.k) == (6, 5, 0)
+    p = hxt.Product(torch.empty(0, 3, 8, dtype=BF16), torch.empty(5, 8, dtype=BF16), c=torch.empty(0, 3, 5, dtype=BF16))
+    assert (p.c.m, p.c.n, p.c.k) == (0, 5, 8)
+    g = hxt.ProductGrad(torch.empty(2, 3, 0, dtype=BF16), b=torch.empty(0, 8, dtype=BF16), da=torch.empty(2, 3, 8, dtype=BF16))
+    assert (g.c.m, g.c.n, g.c.k) == (6, 0, 8)
+    with pytest.raises(ValueError):
+        hxt.Product(a, b, c=torch.empty(5, 5, dtype=BF16))
