@@ -236,8 +236,7 @@ struct TileOf {
     }
     // The descriptor of a step's base, and load j of the EACH that bring a tile.  The load is written out because the compiler, where
     // it knows of loads into LDS, waits for all of them before every transposing read; the kernel's own waits and barriers
-    // order them.  It has no register for a result; m0, which the compiler sets anew before any use of its own, says where the
-    // wave's block goes, 16 bytes a lane.
+    // order them.  It has no register for a result; m0 says where the wave's block goes, 16 bytes a lane.
     static __device__ __forceinline__ i32x4 descriptor(const Operand &o, uint32_t row0, uint32_t step)
     {
         const uint64_t base = reinterpret_cast<uint64_t>(o.p) + (ACROSS ? uint64_t(step) * DEPTH * uint64_t(o.stride)
@@ -248,7 +247,10 @@ struct TileOf {
     {
         if (PIECES % THREADS && j * THREADS + int(threadIdx.x) >= PIECES) return;
         const uint32_t to = __builtin_amdgcn_readfirstlane(int(lds + (threadIdx.x >> 6) * BLOCK)) + j * (THREADS / 64) * BLOCK;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at[j]), "s"(from) : "memory");
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"          // (m0 is reserved; naming it keeps the compiler from carrying a value of its own past here)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at[j]), "s"(from) : "memory", "m0");
+#pragma clang diagnostic pop
     }
 
     // Through registers: any alignment, zeros outside the operand.

@@ -1,5 +1,7 @@
 """What the operators at the ends of a stage take and refuse at an edge, through the C ABI and the binding, on the CPU."""
 import ctypes as C
+import os
+import re
 
 import pytest
 import torch
@@ -83,3 +85,16 @@ def test_the_binding_takes_rows_of_no_elements():
     assert (g.c.m, g.c.n, g.c.k) == (6, 0, 8)
     with pytest.raises(ValueError):
         hxt.Product(a, b, c=torch.empty(5, 5, dtype=BF16))
+
+
+def test_assembly_says_that_it_writes_m0():
+    """The compiler may set m0 for itself and rely on it later: a statement that writes it names it among what it changes."""
+    csrc = os.path.join(os.path.dirname(hxt.LIB_PATH), "csrc")
+    writes = 0
+    for name in sorted(os.listdir(csrc)):
+        text = open(os.path.join(csrc, name)).read()
+        for statement in re.findall(r"asm volatile\((.*?)\);", text, flags=re.S):
+            if re.search(r"s_mov_b32 m0\b", statement):
+                writes += 1
+                assert re.search(r':[^:]*"m0"', statement), "%s: %s" % (name, statement)
+    assert writes > 0
