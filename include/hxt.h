@@ -476,7 +476,7 @@ int hxt_unpack_verify_batch(int n, const hxt_plan_t *const *plans, const void *c
  * and in 8 bits   scale = max(max|y| / 448, 2^-126),   q = y / scale    (a row without any value but 0 has q = 0; with a
  * NaN in y, a scale of NaN).  Any of the outputs h, y, q may be NULL, not all of them if there are rows.  1 <= cols <= 32768 and
  * rows < 2^31 (HXT_EUNSUPPORTED above).
- * h may be x's or residual's matrix, and so may y if h does not go there. */
+ * h may be x's or residual's matrix, and so may y if h is NULL. */
 typedef struct {
     int64_t rows, cols;
     hxt_dtype_t dtype;              /* HXT_BF16 or HXT_F32: of x, residual, weight, h and y */

@@ -13,7 +13,8 @@ template <typename T, int G, int EPT, bool PACK>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm_grad(NormGradArgs a)
 {
     constexpr uint32_t V = Number<T>::V, NV = EPT / V, THREADS = G < 256 ? 256 : G, PER = THREADS / G;
-    __shared__ float part[2][16], part_s[16], part_g[16], joined[PER > 1 ? G * EPT : 1];
+    __shared__ float part[2][16], part_s[16], part_g[16];
+    __shared__ __attribute__((aligned(16))) float joined[PER > 1 ? G * EPT : 1];
     __shared__ uint32_t part_top[16];
     const uint32_t t = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / (G / 64);
     const uint64_t rb = uint64_t(a.cols) * sizeof(T);
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_norm_grad(NormGradArgs a)
 template <int SLICES>
 __global__ __launch_bounds__(16 * SLICES) void k_column_sums(const float *__restrict__ partial, uint32_t n, uint32_t cols, const float *add, float *to)
 {
-    __shared__ float part[SLICES][64];
+    __shared__ __attribute__((aligned(16))) float part[SLICES][64];
     typedef f32x4 f32x4_any __attribute__((aligned(4)));
     const uint32_t quad = threadIdx.x & 15, slice = threadIdx.x >> 4, col = blockIdx.x * 64 + quad * 4;
     f32x4 s = {0, 0, 0, 0};

@@ -54,10 +54,6 @@ typedef u32x2 u32x2_any __attribute__((aligned(1)));
 // ---- vectors of a row -----------------------------------------------------------------
 // Vector v of a row has n elements, V of them or, at the row's end, fewer.
 
-#ifndef NTS
-#define NTS true
-#define NTL true
-#endif
 template <typename T, bool NT = false>
 __device__ __forceinline__ u32x4 load_row(const uint8_t *row, uint32_t v, uint32_t n)
 {

@@ -356,14 +356,15 @@ __device__ __forceinline__ void store_part(float *part, uint32_t rows, uint32_t 
     if (n + 2 < cols) at[2] = v.z;
 }
 
-// One instruction's (e4m3) or two (bf16) on 16 x 16 results: c += of 128 bytes a row, lo and hi.
-template <Factor F>
-__device__ __forceinline__ void multiply_step(f32x4 &c, const u32x4 (&q)[2], const u32x4 (&p)[2])
+// 16 x 16 results: c += of DEEP times 64 bytes a row; e4m3's instruction takes 128.
+template <Factor F, int DEEP>
+__device__ __forceinline__ void multiply_pieces(f32x4 &c, const u32x4 (&q)[DEEP], const u32x4 (&p)[DEEP])
 {
     if constexpr (F == F_BF16) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q[h]), __builtin_bit_cast(bf16x8, p[h]), c, 0, 0, 0);
+        for (int h = 0; h < DEEP; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q[h]), __builtin_bit_cast(bf16x8, p[h]), c, 0, 0, 0);
     } else {
+        static_assert(DEEP == 2);
         auto both = [](const u32x4 (&v)[2]) { return i32x8{int(v[0].x), int(v[0].y), int(v[0].z), int(v[0].w), int(v[1].x), int(v[1].y), int(v[1].z), int(v[1].w)}; };
         c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(q), both(p), c, 0, 0, 0, 0, 0, 0);
     }
@@ -439,13 +440,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs a)
         to[J][D] = TileQ::fragment(from + TileP::BYTES, q_first, J, PH / PARTS + D);
     };
     auto multiply = [&]<int PH, int I, int J>(const u32x4 (&pp)[PI][DEEP], const u32x4 (&qq)[RN][DEEP]) {
-        f32x4 &c = acc[PH % PARTS * PI + I][J];
-        if constexpr (F == F_BF16) {
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qq[J][0]), __builtin_bit_cast(bf16x8, pp[I][0]), c, 0, 0, 0);
-        } else {
-            auto both = [](const u32x4 &lo, const u32x4 &hi) { return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; };
-            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(qq[J][0], qq[J][DEEP - 1]), both(pp[I][0], pp[I][DEEP - 1]), c, 0, 0, 0, 0, 0, 0);
-        }
+        multiply_pieces<F>(acc[PH % PARTS * PI + I][J], qq[J], pp[I]);
     };
     constexpr int READS_P = PI * DEEP, READS_Q = RN * DEEP, MATRIX = PI * RN, LOADS = TileP::EACH + TileQ::EACH;
     uint32_t step = first;
@@ -618,7 +613,7 @@ __global__ __launch_bounds__(256) void k_product_ring(ProductArgs a)
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int j = 0; j < R; ++j) multiply_step<F>(acc[i][j], q[j], p[i]);
+            for (int j = 0; j < R; ++j) multiply_pieces<F>(acc[i][j], q[j], p[i]);
     };
     uint32_t at_p[Tile::EACH], at_q[Tile::EACH];
     Tile::offsets(a.p, m0, at_p);
@@ -711,7 +706,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product_rows(ProductArgs a)
     auto use = [&](uint32_t b, const u32x4 (&xs)[UNROLL][2], const u32x4 (&ys)[UNROLL][2]) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
-            if (wave + WAVES * (b * UNROLL + u) < pieces) multiply_step<F>(acc, ys[u], xs[u]);
+            if (wave + WAVES * (b * UNROLL + u) < pieces) multiply_pieces<F>(acc, ys[u], xs[u]);
     };
     if (batches) load(0, x[0], y[0]);
     for (uint32_t b = 0; b < batches; b += 2) {
@@ -731,7 +726,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product_rows(ProductArgs a)
             return __builtin_bit_cast(u32x4, e);
         };
         const u32x4 xs[2] = {part(at_a, 0), part(at_a, 1)}, ys[2] = {part(at_b, 0), part(at_b, 1)};
-        multiply_step<F>(acc, ys, xs);
+        multiply_pieces<F>(acc, ys, xs);
     }
     *reinterpret_cast<f32x4 *>(parts + (wave * 16 + r) * PITCH + 4 * g) = acc;       // row l % 16, columns 4 (l / 16) .. + 3
     __syncthreads();
