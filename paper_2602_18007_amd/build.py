@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libhxt.so")
 SOURCES = [os.path.join(PKG, "csrc", f) for f in ("hxt_device.hip", "hxt_transpose.hip", "hxt_transpose_span.hip", "hxt_message_pack.hip",
                                                       "hxt_message_unpack.hip", "hxt_norm.hip", "hxt_norm_grad.hip", "hxt_product.hip", "hxt_plan.cpp")]
-HEADERS = [os.path.join(PKG, "csrc", f) for f in ("hxt_internal.h", "hxt_kernels.h", "hxt_launch.h", "hxt_norm_kernels.h", "hxt_operators.h", "hxt_product_kernels.h", "hxt_rules.h")] + \
+HEADERS = [os.path.join(PKG, "csrc", f) for f in ("hxt_internal.h", "hxt_kernels.h", "hxt_launch.h", "hxt_norm_kernels.h", "hxt_operators.h", "hxt_product_kernels.h", "hxt_product_rules.h",
+                                                      "hxt_rules.h")] + \
           [os.path.join(ROOT, "include", "hxt.h")]
 
 

@@ -14,6 +14,7 @@
 #define HXT_PRODUCT_KERNELS_H
 
 #include "hxt_operators.h"
+#include "hxt_product_rules.h"
 
 namespace hxt {
 
@@ -188,7 +189,6 @@ __device__ __forceinline__ void pad_message(const Epilogue &e)
 
 // ---- operand tiles in LDS ------------------------------------------------------------------
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-constexpr int kStep = 128;        // bytes of a row per step, of operands along; across: kStep / 2 rows
 
 // One operand's tile: T rows of m or n, in LDS as the direct loads leave it, in blocks of 1024 bytes that one wave writes.
 //   along:  T rows of 128 bytes; 16-byte piece c of row r lies at place c ^ turn(r), so that the 16 rows that a fragment load
