@@ -4,8 +4,9 @@
 // registers and walks the contraction in steps of 128 bytes a row (64 bf16, 128 e4m3).  A step's two operand tiles lie in
 // LDS, twice, so that the next step's loads run under this step's matrix instructions.
 //
-// Bound by the matrix cores, at the clock that the power limit leaves: 4096 x 4096 x 14336 bf16 in 256 x 256 tiles 341 to 352 us (1370 to
-// 1410 TFLOP/s), 8192 x 8192 x 8192 745, with operands of zeros 616.  16 x 16 x 32 instructions rather than 32 x 32 x 16, whose accumulators'
+// Bound by the matrix cores, at the clock that the power limit leaves: 4096 x 4096 x 14336 bf16 in 256 x 256 tiles 341 to 365 us on one card
+// and another (1320 to 1410 TFLOP/s); the matrix pipes are busy for 68% of the cycles, at 2.04 GHz, and with operands of zeros 63% at 2.43 GHz
+// (303 us); 8192 x 8192 x 8192 745, of zeros 616.  16 x 16 x 32 instructions rather than 32 x 32 x 16, whose accumulators'
 // traffic costs power (zeros 599, data 821 us).
 //
 // An operand is either along (its rows are m or n, the contraction index is adjacent) or across (its rows are the contraction
@@ -315,8 +316,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // Tiles in an order that keeps neighbours on one XCD's L2: workgroups go to the eight XCDs in turn, so each XCD takes a run of
-// consecutive tiles, and consecutive tiles are blocks 8 tiles high (4096 x 14336 x 4096 367 us, 4 high 360, 16 high 395; 4096 x 4096 x
-// 14336 337, 340, 351).
+// consecutive tiles, and consecutive tiles are blocks 8 tiles high (bf16 4096 x 4096 x 14336 341 us, 4 high 342, 16 high 355;
+// 4096 x 14336 x 4096 381, 377 and 404, of 8 bits 204, 200 and 218).
 __device__ __forceinline__ void tile_at(uint32_t id, uint32_t all, uint32_t tm, uint32_t tn, uint32_t &i, uint32_t &j)
 {
     const uint32_t xcd = id & 7, each = all >> 3, more = all & 7;

@@ -28,8 +28,7 @@ inline uint32_t up(uint64_t n, uint64_t to) { return uint32_t((n + to - 1) / to)
 //   rounds), one a CU 0.65; through registers (operands not in vectors) 1.6; the ring of 64 x 64, one a CU, 0.42 (64 x 14336 x
 //   4096: 27.8 us in one round of 64 steps; as 128 x 128 tiles in four parts 34.9).  A round's ramp and end 4 (ring 2.5); joining
 //   the parts 4 and what they take to be written and read at 5 TB/s.  Where whole rounds of 256 x 256 tiles leave few, these go as
-//   256 x 128 in a launch of their own (8 bits, 4096 x 14336 x 4096: 213 -> 202 us; bf16 387 -> 385, where the clock gives back what
-//   a half-empty round leaves).
+//   256 x 128 in a launch of their own (4096 x 14336 x 4096: 8 bits 214 -> 204 us, bf16 396 -> 381).
 //   Up to 4 rows (16 where the ring cannot serve them) k_product_rows: 1 x 4096 x 14336 23.6 us against 27.5 as a ring in four
 //   parts; 8 x 14336 x 4096 29.5 against 26.
 inline Shape shape_for(int64_t m, int64_t n, int64_t depth, int64_t es, bool along, bool direct)
